@@ -1,0 +1,546 @@
+"""The operators of a learner next to the sequence layer, as measurable cases over their public Python entry points.
+
+  gated   the gated linear recurrence over a batch of sequences: "forward", "train" (forward and gradient pass) and
+          "step" (one token of every sequence, as acting needs it)
+  policy  the clipped policy loss with a KL term and an entropy bonus, from logits: "forward" (evaluation), "train"
+          (loss and gradient with respect to the logits)
+  adamw   one optimizer step over a list of parameters, states in 32 or in 8 bits
+
+`own` false: the plain form, elementary torch operations in 32 bits, rounded once at the end.  `own` true: the calls that a
+user makes.  Both work on what `prepare` gives; the optimizer updates its tensors in place on either side.
+"""
+import math
+
+import torch
+
+own = False
+
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+BYTES = {"f32": 4, "bf16": 2, "f16": 2}
+CLIP_LOW, CLIP_HIGH = 0.2, 0.25
+LR, BETA1, BETA2, EPS, DECAY = 3e-4, 0.9, 0.999, 1e-8, 0.01
+BLOCK = 256                          # elements that share a scale where states are held in 8 bits
+
+MAX_GATED = 128 * 256 * 1024         # elements, cost of a draw: of the largest listed cases
+MAX_LOGITS = 4096 * 65536
+MAX_PARAMETERS = 100_000_000
+
+
+def _gated(name, form, Bt, L, D, dtype="f32", layout="dense", linear=False, p_reset=0.0, first=False, h0=False, slow=False):
+    return {"name": name, "op": "gated", "form": form, "Bt": Bt, "L": L, "D": D, "dtype": dtype, "layout": layout,
+            "linear": linear, "p_reset": p_reset, "first": first, "h0": h0, "slow": slow}
+
+
+def _policy(name, form, N, K, dtype="f32", pad=0, masked=0.0, idle=0.0, kl=0.0, entropy=0.0):
+    return {"name": name, "op": "policy", "form": form, "N": N, "K": K, "dtype": dtype, "pad": pad, "masked": masked,
+            "idle": idle, "kl": kl, "entropy": entropy}
+
+
+def _adamw(name, tensors, layers, H, P, dtype="f32", gdtype="f32", bits=32, scaled=False, align=64):
+    return {"name": name, "op": "adamw", "tensors": tensors, "layers": layers, "H": H, "P": P, "dtype": dtype, "gdtype": gdtype,
+            "bits": bits, "scaled": scaled, "align": align}
+
+
+def listed():
+    return [
+        # acting: one step of 16 environments, where latency counts
+        _gated("gated_step_acting", "step", 16, 1, 512, p_reset=0.02, h0=True),
+        # the replay batch of one world-model update
+        _gated("gated_train_worldmodel", "train", 16, 256, 512, p_reset=0.01, first=True),
+        # few, very long sequences with slow decay
+        _gated("gated_train_long", "train", 4, 4096, 256, dtype="bf16", p_reset=0.001, first=True, slow=True),
+        # windows of no convenient length, a width that no vector divides
+        _gated("gated_train_ragged", "train", 20, 300, 250, dtype="f16", p_reset=0.02, h0=True),
+        # a large update: gate and input are the halves of one projection's output
+        _gated("gated_train_large", "train", 128, 256, 1024, dtype="bf16", layout="halves", p_reset=0.01, first=True),
+        # log-probabilities of a few sampled tokens over a large vocabulary
+        _policy("policy_forward_few", "forward", 16, 65536, dtype="bf16"),
+        # a policy over 32 discrete actions, some of them illegal, over a batch of imagined steps
+        _policy("policy_train_actions", "train", 16384, 32, masked=0.3, entropy=3e-3),
+        # rows of no convenient length in a padded array, a tenth of them padding
+        _policy("policy_train_ragged", "train", 1021, 5003, pad=13, idle=0.1, kl=0.05, entropy=1e-3),
+        # fine-tuning on token sequences: 4096 tokens, a large vocabulary
+        _policy("policy_train_vocabulary", "train", 4096, 65536, dtype="bf16", idle=0.05, kl=0.05),
+        # the parameters of one narrow layer, where latency counts
+        _adamw("adamw_layer", 6, 1, 32, 32),
+        # two layers and the dense layers around them, at the width of the vision task
+        _adamw("adamw_worldmodel", 24, 2, 1024, 512, scaled=True),
+        # a large model, gradients in bf16, states in 8 bits
+        _adamw("adamw_large_8bit", 96, 16, 2048, 1024, gdtype="bf16", bits=8, scaled=True),
+    ]
+
+
+def _log_uniform(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def _width(rng, lo, hi):
+    w = _log_uniform(rng, lo, hi)
+    return max(64, w // 64 * 64) if rng.random() < 0.5 else w
+
+
+def draw(rng):
+    op = rng.choice(("gated", "gated", "policy", "adamw"))
+    dtype = rng.choice(("f32", "bf16", "f16"))
+    if op == "gated":
+        form = rng.choice(("forward", "train", "train", "train", "step"))
+        flags = {"linear": rng.random() < 0.25, "p_reset": rng.choice((0.0, 0.001, 0.01, 0.02)), "h0": rng.random() < 0.5,
+                 "layout": rng.choice(("dense", "halves", "time"))}
+        if form == "step":
+            return _unnamed(_gated("", form, _log_uniform(rng, 1, 4096), 1, _width(rng, 16, 4096), dtype, **flags))
+        while True:
+            L, D = _log_uniform(rng, 2, 16384), _width(rng, 16, 4096)
+            Bt = _log_uniform(rng, 1, 2048)
+            if 1 << 14 <= Bt * L * D <= MAX_GATED:
+                break
+        return _unnamed(_gated("", form, Bt, L, D, dtype, first=rng.random() < 0.5, slow=L >= 1024, **flags))
+    if op == "policy":
+        while True:
+            N, K = _log_uniform(rng, 1, 65536), _log_uniform(rng, 2, 131072)
+            if 1 << 12 <= N * K <= MAX_LOGITS // (2 if dtype == "f32" else 1):
+                break
+        K = max(64, K // 64 * 64) if K >= 64 and rng.random() < 0.4 else K
+        return _unnamed(_policy("", rng.choice(("forward", "train", "train")), N, K, dtype, pad=rng.choice((0, 0, 5, 64)),
+                                masked=rng.choice((0.0, 0.0, 0.3)), idle=rng.choice((0.0, 0.1)), kl=rng.choice((0.0, 0.05)),
+                                entropy=rng.choice((0.0, 1e-3))))
+    while True:
+        layers = rng.randint(1, 16)
+        case = _unnamed(_adamw("", rng.randint(1, 8) * layers, layers, _width(rng, 16, 2048), _width(rng, 16, 1024), dtype=dtype,
+                               gdtype=dtype if dtype != "f32" else rng.choice(("f32", "bf16", "f16")), bits=rng.choice((8, 32)),
+                               scaled=rng.random() < 0.5, align=rng.choice((1, 64))))
+        if sum(_sizes(case)) <= MAX_PARAMETERS:
+            return case
+
+
+def _unnamed(case):
+    del case["name"]
+    return case
+
+
+def _sizes(case):
+    """Element counts of the parameters: those of the layers in turn, the complex ones as pairs."""
+    H, P = case["H"], case["P"]
+    layer = (2 * P, 2 * P * H, 2 * H * P, H, P, H * H, 4 * H * H, H + 1)
+    per = [layer[i % len(layer)] for i in range(max(1, case["tensors"] // case["layers"]))]
+    return (per * case["layers"])[:case["tensors"]]
+
+
+# ------------------------------------------------------------------ inputs
+def prepare(case, seed):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    normal = lambda *shape: torch.randn(shape, generator=gen, device="cuda")
+    uniform = lambda lo, hi, *shape: torch.rand(shape, generator=gen, device="cuda") * (hi - lo) + lo
+    return _PREPARE[case["op"]](case, gen, normal, uniform)
+
+
+def _prepare_gated(case, gen, normal, uniform):
+    Bt, L, D, dt = case["Bt"], case["L"], case["D"], DTYPES[case["dtype"]]
+    step = case["form"] == "step"
+    shape = (Bt, D) if step else (Bt, L, D)
+    z = normal(*shape) + (5.0 if case["slow"] else 2.0)               # decay over 150 or 8 steps
+    u = normal(*shape)
+    if case["linear"]:
+        z, u = torch.sigmoid(z), u * 0.2
+    if case["layout"] == "halves":
+        both = torch.cat((z, u), -1).to(dt)
+        z, u = both[..., :D], both[..., D:]
+    elif case["layout"] == "time" and not step:
+        z, u = (t.to(dt).transpose(0, 1).contiguous().transpose(0, 1) for t in (z, u))
+    else:
+        z, u = z.to(dt), u.to(dt)
+    flags = uniform(0, 1, *shape[:-1]) < case["p_reset"]
+    if case["first"]:
+        flags[:, 0] = True
+    s = {"case": case, "gate": z, "u": u, "is_first": flags.to(torch.uint8) if case["first"] or case["p_reset"] > 0 else None,
+         "h0": normal(Bt, D) if case["h0"] or step else None}
+    if case["form"] == "train":
+        s["dh"] = torch.empty_like(u).copy_(normal(*shape))
+        s["dh_last"] = normal(Bt, D) if case["h0"] else None
+    return s
+
+
+def _prepare_policy(case, gen, normal, uniform):
+    N, K = case["N"], case["K"]
+    x = (normal(N, K + case["pad"]) * 2.0).to(DTYPES[case["dtype"]])[:, :K]
+    action = torch.randint(K, (N,), generator=gen, device="cuda")
+    if case["masked"] > 0:                                            # illegal actions; the one taken is legal
+        illegal = uniform(0, 1, N, K) < case["masked"]
+        illegal[torch.arange(N, device="cuda"), action] = False
+        x.masked_fill_(illegal, -math.inf)
+    logp = _log_softmax(x).gather(1, action[:, None])[:, 0]
+    weight = (uniform(0, 1, N) >= case["idle"]).float()
+    return {"case": case, "logits": x, "action": action, "logp_old": logp + 0.2 * normal(N), "advantage": normal(N),
+            "weight": weight / weight.sum().clamp(min=1.0), "logp_ref": logp + 0.3 * normal(N) if case["kl"] > 0 else None}
+
+
+def _starts(sizes, align):
+    """Where tensors of these sizes start in one buffer, each at a multiple of `align`, and the buffer's length."""
+    starts, at = [], 0
+    for n in sizes:
+        starts.append(at)
+        at += -(-n // align) * align
+    return starts, at
+
+
+def _prepare_adamw(case, gen, normal, uniform):
+    # parameters, gradients and states lie in one buffer each, as a program keeps them that reduces or saves them in one go
+    sizes, dt, gdt = _sizes(case), DTYPES[case["dtype"]], DTYPES[case["gdtype"]]
+    starts, total = _starts(sizes, case["align"])
+    s = {"case": case, "all": {}, "m_scale": None, "v_scale": None, "step": 100,
+         "grad_scale": uniform(0.5, 1.0, 1) if case["scaled"] else None}
+
+    def keep(name, buffer):
+        s["all"][name] = buffer
+        s[name] = [buffer[at:at + n] for at, n in zip(starts, sizes)]
+
+    keep("params", (normal(total) * 0.05).to(dt))
+    keep("grads", (normal(total) * 0.01).to(gdt))
+    if case["bits"] == 32:
+        keep("m", normal(total) * 2e-3)
+        keep("v", uniform(0.2, 2.0, total) * 1e-4)
+        return s
+    codes = torch.randint(0, 0x7f, (total,), generator=gen, device="cuda", dtype=torch.uint8)
+    keep("m", codes + torch.randint(0, 2, (total,), generator=gen, device="cuda", dtype=torch.uint8) * 128)
+    keep("v", torch.randint(100, 256, (total,), generator=gen, device="cuda", dtype=torch.uint8))
+    s["m_scale"] = [uniform(0.5, 1.5, -(-n // BLOCK)) * 1e-5 for n in sizes]
+    s["v_scale"] = [uniform(0.5, 1.5, -(-n // BLOCK)) * 1e-2 for n in sizes]
+    keep("m_values", torch.zeros(total, device="cuda"))               # what the states stand for: a checkpoint
+    keep("v_values", torch.zeros(total, device="cuda"))
+    return s
+
+
+_PREPARE = {"gated": _prepare_gated, "policy": _prepare_policy, "adamw": _prepare_adamw}
+
+
+# ------------------------------------------------------------------ one pass
+def run(state):
+    return (_OWN if own else _PLAIN)[state["case"]["op"]](state)
+
+
+def _own_gated(s):
+    from paper_2502_20168_amd import learn
+    c = s["case"]
+    if c["form"] == "step":
+        y, h = learn.ssm_gated_step(s["gate"], s["u"], s["h0"], s["is_first"], linear=c["linear"])
+        return {"h": y, "h_last": h}
+    train = c["form"] == "train"
+    f = learn.ssm_gated_scan_fwd(s["gate"], s["u"], s["is_first"], s["h0"], linear=c["linear"], want_carry=train)
+    out = {"h": f["h"], "h_last": f["h_last"]}
+    if train:
+        b = learn.ssm_gated_scan_bwd(s["gate"], s["u"], s["is_first"], s["h0"], f["carry"], s["dh"], s["dh_last"],
+                                     linear=c["linear"], want_dh0=c["h0"])
+        out.update((k, b[k]) for k in ("dgate", "du") + (("dh0",) if c["h0"] else ()))
+    return out
+
+
+def _own_policy(s):
+    from paper_2502_20168_amd import learn
+    c = s["case"]
+    call = learn.ssm_policy_loss_grad if c["form"] == "train" else learn.ssm_policy_loss_fwd
+    r = call(s["logits"], s["action"], s["logp_old"], s["advantage"], s["weight"], s["logp_ref"], clip_low=CLIP_LOW,
+             clip_high=CLIP_HIGH, kl_coef=c["kl"], entropy_coef=c["entropy"])
+    return {k: r[k] for k in ("loss", "logp", "entropy") + (("dlogits",) if c["form"] == "train" else ())}
+
+
+def _own_adamw(s):
+    from paper_2502_20168_amd import learn
+    learn.ssm_adamw_step(s["params"], s["grads"], s["m"], s["v"], s["m_scale"], s["v_scale"], lr=LR, beta1=BETA1, beta2=BETA2,
+                         eps=EPS, weight_decay=DECAY, step=s["step"], grad_scale=s["grad_scale"])
+    if s["case"]["bits"] == 8:
+        learn.ssm_adamw_values(s["m"], s["v"], s["m_scale"], s["v_scale"], s["m_values"], s["v_values"])
+    return _updated(s)
+
+
+def _updated(s):
+    kept = ("params", "m", "v") if s["case"]["bits"] == 32 else ("params", "m_values", "v_values")
+    return {k: s["all"][k] for k in kept}
+
+
+_OWN = {"gated": _own_gated, "policy": _own_policy, "adamw": _own_adamw}
+
+
+# ------------------------------------------------------------------ the plain forms
+def _scan(a, b):
+    """x_t = a_t x_{t-1} + b_t along dimension 1 by doubling."""
+    d, L = 1, b.shape[1]
+    while d < L:
+        b = torch.cat((b[:, :d], b[:, d:] + a[:, d:] * b[:, :-d]), 1)
+        a = torch.cat((a[:, :d], a[:, d:] * a[:, :-d]), 1)
+        d *= 2
+    return b
+
+
+def _plain_gated(s):
+    c = s["case"]
+    z, u = s["gate"].float(), s["u"].float()
+    f = z if c["linear"] else 1.0 / (1.0 + torch.exp(-z))
+    i = None if c["linear"] else 1.0 / (1.0 + torch.exp(z))           # 1 - f without cancellation
+    b = u if c["linear"] else i * u
+    keep = None if s["is_first"] is None else (s["is_first"] == 0).float()[..., None]
+    a = f if keep is None else f * keep
+    if c["form"] == "step":
+        h = a * s["h0"] + b
+        return {"h": h.to(s["u"].dtype), "h_last": h}
+    if s["h0"] is not None:
+        b = torch.cat((b[:, :1] + a[:, :1] * s["h0"][:, None], b[:, 1:]), 1)
+    h = _scan(a, b)
+    out = {"h": h.to(s["u"].dtype), "h_last": h[:, -1].clone()}
+    if c["form"] == "forward":
+        return out
+    g = s["dh"].float()
+    if s["dh_last"] is not None:
+        g = torch.cat((g[:, :-1], g[:, -1:] + s["dh_last"][:, None]), 1)
+    up = torch.cat((a[:, 1:], torch.zeros_like(a[:, :1])), 1)
+    chi = _scan(up.flip(1), g.flip(1)).flip(1)
+    before = torch.zeros_like(h[:, :1]) if s["h0"] is None else s["h0"][:, None]
+    before = torch.cat((before, h[:, :-1]), 1)
+    if keep is not None:
+        before = before * keep
+    if c["linear"]:
+        dz, du = before * chi, chi
+    else:
+        dz, du = f * i * (before - u) * chi, i * chi
+    out.update(dgate=dz.to(s["gate"].dtype), du=du.to(s["u"].dtype))
+    if c["h0"]:
+        out["dh0"] = a[:, 0] * chi[:, 0]
+    return out
+
+
+def _log_softmax(x):
+    x = x.float()
+    d = x - x.amax(1, keepdim=True)
+    return d - torch.log(torch.exp(d).sum(1, keepdim=True))
+
+
+def _plain_policy(s):
+    c = s["case"]
+    lp = _log_softmax(s["logits"])
+    p = torch.exp(lp)
+    plp = torch.where(p > 0, p * lp, torch.zeros_like(lp))
+    used, w, A = s["weight"] != 0, s["weight"], s["advantage"]
+    zero = torch.zeros_like(w)
+    entropy = -plp.sum(1)
+    logp = lp.gather(1, s["action"][:, None])[:, 0]
+    rho = torch.exp(logp - s["logp_old"])
+    raw, clipped = rho * A, rho.clamp(1.0 - CLIP_LOW, 1.0 + CLIP_HIGH) * A
+    row = -torch.minimum(raw, clipped) - c["entropy"] * entropy
+    g = torch.where(raw <= clipped, -raw, zero)
+    if s["logp_ref"] is not None:
+        d = s["logp_ref"] - logp
+        e = torch.exp(d)
+        row, g = row + c["kl"] * (e - d - 1.0), g + c["kl"] * (1.0 - e)
+    out = {"loss": torch.where(used, w * row, zero).sum(), "logp": torch.where(used, logp, zero), "entropy": torch.where(used, entropy, zero)}
+    if c["form"] == "train":
+        dx = c["entropy"] * (plp + p * entropy[:, None]) - p * g[:, None]
+        dx.scatter_add_(1, s["action"][:, None], g[:, None])
+        out["dlogits"] = torch.where(used[:, None], w[:, None] * dx, torch.zeros_like(dx)).to(s["logits"].dtype)
+    return out
+
+
+def _padded_blocks(t):
+    return torch.nn.functional.pad(t, (0, -t.numel() % BLOCK)).view(-1, BLOCK)
+
+
+def _encode(x, mantissa, lowest):
+    """Values of 4 exponent and `mantissa` bits, the smallest normal one 2**lowest, round to nearest even: code of |x|."""
+    e = torch.where(x > 0, torch.frexp(x)[1].clamp(min=lowest + 1) - 1, lowest)
+    q = torch.round(torch.ldexp(x, mantissa - e))
+    return ((e - lowest) * 2 ** mantissa + q).to(torch.int32)
+
+
+def _decode(code, mantissa, lowest):
+    code = code.to(torch.int32)
+    e = (code >> mantissa).clamp(min=1)
+    return torch.ldexp((code - ((e - 1) << mantissa)).float(), e - 1 + lowest - mantissa)
+
+
+def _values(code, scale, signed):
+    if signed:
+        x = _decode(code & 127, 3, -6)
+        x = torch.where(code >= 128, -x, x)
+    else:
+        x = _decode(code, 4, -14)
+    return (_padded_blocks(x) * scale[:, None]).view(-1)[:code.numel()]
+
+
+def _store(x, code, scale, signed):
+    """8 bits of x under one scale per block; returns the values they stand for."""
+    top = 448.0 if signed else 1.9375
+    b = _padded_blocks(x)
+    big = b.abs().amax(1)
+    big = torch.where(big < 2.0 ** -100, torch.zeros_like(big), big)
+    inv = torch.where(big > 0, torch.full_like(big, top) / big, big)
+    n = x.numel()
+    y = (b.abs() * inv[:, None]).view(-1)[:n]
+    k = _encode(y, 3, -6) if signed else _encode(y, 4, -14)
+    if signed:
+        k = k + 128 * torch.signbit(x).int()
+    else:
+        k = torch.where(y > 0, k.clamp(min=1), k)         # a positive second moment never becomes zero
+    code.copy_(k)
+    scale.copy_(big / top)
+    return _values(code, scale, signed)
+
+
+def _plain_adamw(s):
+    c1, c2 = 1.0 - BETA1 ** s["step"], 1.0 - BETA2 ** s["step"]
+    eight = s["case"]["bits"] == 8
+    for k, (p, grad, m, v) in enumerate(zip(s["params"], s["grads"], s["m"], s["v"])):
+        g = grad.float()
+        if s["grad_scale"] is not None:
+            g = g * s["grad_scale"]
+        m1 = _values(m, s["m_scale"][k], True) if eight else m
+        v1 = _values(v, s["v_scale"][k], False) ** 2 if eight else v
+        m1 = m1 * BETA1 + g * (1.0 - BETA1)
+        v1 = v1 * BETA2 + (g * g) * (1.0 - BETA2)
+        root = torch.sqrt(v1)
+        p.copy_(p.float() * (1.0 - LR * DECAY) - (LR / c1) * (m1 / (root / math.sqrt(c2) + EPS)))
+        if eight:
+            s["m_values"][k].copy_(_store(m1, m, s["m_scale"][k], True))
+            s["v_values"][k].copy_(_store(root, v, s["v_scale"][k], False) ** 2)
+        else:
+            m.copy_(m1)
+            v.copy_(v1)
+    return _updated(s)
+
+
+_PLAIN = {"gated": _plain_gated, "policy": _plain_policy, "adamw": _plain_adamw}
+
+
+# ------------------------------------------------------------------ compulsory work
+def work(case):
+    """Bytes and operations of one pass: each input read once, each output written once."""
+    if case["op"] == "gated":
+        rows = case["Bt"] * case["L"]
+        n, e = rows * case["D"], BYTES[case["dtype"]]
+        flags = rows if case["first"] or case["p_reset"] > 0 else 0
+        ends = 4 * case["Bt"] * case["D"] * (2 if case["h0"] or case["form"] == "step" else 1)
+        forward = {"bytes": 3 * e * n + flags + ends, "flops": 8 * n}
+        if case["form"] != "train":
+            return forward
+        # gate and u once for both directions; dh in, dgate and du out; dh0 and dh_last where there is an h0
+        return {"bytes": 6 * e * n + flags + ends + (8 * case["Bt"] * case["D"] if case["h0"] else 0), "flops": 22 * n}
+    if case["op"] == "policy":
+        n, e = case["N"] * case["K"], BYTES[case["dtype"]]
+        rows = case["N"] * (8 + 4 * 5 + (4 if case["kl"] > 0 else 0))
+        train = case["form"] == "train"
+        return {"bytes": e * n * (2 if train else 1) + rows, "flops": (14 if train else 8) * n}
+    n = sum(_sizes(case))
+    state = 16 if case["bits"] == 32 else 4 + 8 + 16 / BLOCK          # 8 bits: the values are written out as well
+    return {"bytes": int(n * (2 * BYTES[case["dtype"]] + BYTES[case["gdtype"]] + state)), "flops": 16 * n}
+
+
+# ------------------------------------------------------------------ the definitions in 64 bits
+def exact(case, seed):
+    return _EXACT[case["op"]](prepare(case, seed))
+
+
+def _exact_gated(s):
+    c = s["case"]
+    if c["Bt"] * c["L"] * c["D"] * 8 * 9 > 60e9:
+        return None
+    z, u = s["gate"].double(), s["u"].double()
+    step = c["form"] == "step"
+    if step:
+        z, u = z[:, None], u[:, None]
+    Bt, L, D = z.shape
+    first = torch.zeros(Bt, L, dtype=torch.bool, device=z.device) if s["is_first"] is None else s["is_first"].view(Bt, L) != 0
+    decay = z if c["linear"] else torch.sigmoid(z)
+    inp = u if c["linear"] else torch.sigmoid(-z) * u
+    cut = first[..., None]
+    h = torch.empty_like(z)
+    state = torch.zeros(Bt, D, dtype=z.dtype, device=z.device) if s["h0"] is None else s["h0"].double()
+    for t in range(L):
+        state = torch.where(cut[:, t], inp[:, t], decay[:, t] * state + inp[:, t])
+        h[:, t] = state
+    if step:
+        return {"h": h[:, 0], "h_last": state}
+    out = {"h": h, "h_last": state}
+    if c["form"] == "forward":
+        return out
+    dz, du = torch.empty_like(z), torch.empty_like(z)
+    start = torch.zeros_like(state) if s["h0"] is None else s["h0"].double()
+    back = torch.zeros_like(state) if s["dh_last"] is None else s["dh_last"].double()
+    for t in reversed(range(L)):
+        chi = s["dh"][:, t].double() + back
+        prev = h[:, t - 1] if t else start
+        prev = torch.where(cut[:, t], torch.zeros_like(prev), prev)
+        if c["linear"]:
+            dz[:, t], du[:, t] = prev * chi, chi
+        else:
+            du[:, t] = torch.sigmoid(-z[:, t]) * chi
+            dz[:, t] = decay[:, t] * torch.sigmoid(-z[:, t]) * (prev - u[:, t]) * chi
+        back = torch.where(cut[:, t], torch.zeros_like(chi), decay[:, t] * chi)
+    out.update(dgate=dz, du=du)
+    if c["h0"]:
+        out["dh0"] = back
+    return out
+
+
+def _exact_policy(s):
+    c = s["case"]
+    N, rows = c["N"], max(1, (1 << 27) // c["K"])
+    out = {k: torch.zeros(N, dtype=torch.float64, device="cuda") for k in ("logp", "entropy")}
+    loss = torch.zeros((), dtype=torch.float64, device="cuda")
+    grads = []
+    for lo in range(0, N, rows):
+        part = slice(lo, min(N, lo + rows))
+        x, a, w = s["logits"][part].double(), s["action"][part], s["weight"][part].double()
+        live = w != 0
+        lse = torch.logsumexp(x, 1)
+        prob = torch.exp(x - lse[:, None])
+        logs = torch.where(prob > 0, x - lse[:, None], torch.zeros_like(x))
+        H = -(prob * logs).sum(1)
+        lpa = x[torch.arange(x.shape[0], device=x.device), a] - lse
+        A, ratio = s["advantage"][part].double(), torch.exp(lpa - s["logp_old"][part].double())
+        low, high = 1.0 - CLIP_LOW, 1.0 + CLIP_HIGH
+        held = ((A > 0) & (ratio > high)) | ((A < 0) & (ratio < low))
+        term = torch.where(held, -torch.clamp(ratio, low, high) * A, -ratio * A) - c["entropy"] * H
+        slope = torch.where(held, torch.zeros_like(A), -ratio * A)
+        if s["logp_ref"] is not None:
+            gap = s["logp_ref"][part].double() - lpa
+            term = term + c["kl"] * (torch.expm1(gap) - gap)
+            slope = slope - c["kl"] * torch.expm1(gap)
+        loss = loss + (w * term)[live].sum()
+        out["logp"][part], out["entropy"][part] = lpa * live, H * live
+        if c["form"] == "train":
+            hot = torch.zeros_like(x)
+            hot[torch.arange(x.shape[0], device=x.device), a] = 1.0
+            grads.append((w * live)[:, None] * (slope[:, None] * (hot - prob) + c["entropy"] * prob * (logs + H[:, None])))
+    out["loss"] = loss
+    order = ("loss", "logp", "entropy")
+    out = {k: out[k] for k in order}
+    if c["form"] == "train":
+        out["dlogits"] = torch.cat(grads)
+    return out
+
+
+def _exact_adamw(s):
+    eight = s["case"]["bits"] == 8
+    t = s["step"]
+    new = {k: None if k.endswith("_values") else b.double() for k, b in _updated(s).items()}
+    starts, _ = _starts(_sizes(s["case"]), s["case"]["align"])
+    for k, (p, g, m, v) in enumerate(zip(s["params"], s["grads"], s["m"], s["v"])):
+        g = g.double()
+        if s["grad_scale"] is not None:
+            g = g * s["grad_scale"].double()
+        if eight:
+            # a code's value from its bits: sign, exponent, mantissa
+            c, r = m.long(), v.long()
+            part = lambda code, bits: torch.where(code >> bits == 0, (code % (1 << bits)) * 2.0, (code % (1 << bits)) + float(1 << bits)).double()
+            block = torch.arange(m.numel(), device=m.device) // BLOCK
+            mm = part(c & 127, 3) * 2.0 ** ((c & 127) // 8 - 10.0).double() * s["m_scale"][k].double()[block]
+            m0 = torch.where(c > 127, -mm, mm)
+            v0 = (part(r, 4) * 2.0 ** (r // 16 - 19.0).double() * s["v_scale"][k].double()[block]) ** 2
+        else:
+            m0, v0 = m.double(), v.double()
+        m1, v1 = BETA1 * m0 + (1 - BETA1) * g, BETA2 * v0 + (1 - BETA2) * g ** 2
+        mh, vh = m1 / (1 - BETA1 ** t), v1 / (1 - BETA2 ** t)
+        here = slice(starts[k], starts[k] + p.numel())
+        new["params"][here] = p.double() - LR * DECAY * p.double() - LR * mh / (vh.sqrt() + EPS)
+        if not eight:                                                 # (what 8 bits hold is a step function: no value in 64 bits)
+            new["m"][here], new["v"][here] = m1, v1
+    return new
+
+
+_EXACT = {"gated": _exact_gated, "policy": _exact_policy, "adamw": _exact_adamw}
