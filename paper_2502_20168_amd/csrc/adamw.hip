@@ -1,0 +1,286 @@
+// AdamW over many tensors at once (gfx950), states in 32 or in 8 bits.
+//
+// One pass over parameters, gradients and states.  The tensors of a launch are described in its arguments (no table in memory that would have to be
+// copied and kept); a workgroup finds its tensor among them by counting the first workgroups that are not behind its own.
+//
+// 8 bits: a wavefront holds a block of 256 elements, four to a lane, so the block's largest magnitudes are maxima over its lanes.  Codes are the
+// upper bits of the value as a float whose exponent was moved to the bottom of the range by one exact product: rounding to nearest even is an
+// integer addition there, and small codes become that format's denormal numbers by themselves.  What is rounded to a code is computed in single operations
+// (no contraction), so that a state depends on the formula alone.
+#include "elem.h"
+#include "ssm_internal.h"
+
+#include <cmath>
+
+namespace ssm {
+namespace {
+
+inline bool misaligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
+
+constexpr int ADAMW_TENSORS = 48;            // tensors of a launch
+constexpr int ADAMW_CHUNK = 2048;            // elements of a workgroup: two blocks of 256 per wavefront
+static_assert(ADAMW_CHUNK % (4 * SSM_ADAMW_BLOCK) == 0, "whole blocks per wavefront");
+
+struct AdamwLaunch {
+    ssm_adamw_tensor t[ADAMW_TENSORS];
+    unsigned first[ADAMW_TENSORS];           // first workgroup of every tensor
+    int count;
+    const float *grad_scale, *skip;
+    float decay, beta1, beta2, one_minus_beta1, one_minus_beta2, rate, root2, eps;
+};
+struct ValuesLaunch {
+    ssm_adamw_stored t[ADAMW_TENSORS];
+    unsigned first[ADAMW_TENSORS];
+    int count;
+};
+
+__device__ __forceinline__ int find_tensor(const unsigned *first, int count)
+{
+    int k = 0;
+    for (int i = 1; i < count; ++i) k += blockIdx.x >= first[i];
+    return k;
+}
+
+// Codes.  m: 3 mantissa bits below a bias of 7, largest 448; sqrt(v): 4 below a bias of 15, largest 1.9375.
+template <int MANTISSA, int BIAS> struct Code {
+    static constexpr float DOWN = BIAS == 7 ? 0x1p-120f : 0x1p-112f, UP = BIAS == 7 ? 0x1p120f : 0x1p112f;
+    static __device__ __forceinline__ unsigned of(float magnitude)
+    {
+        const unsigned b = __float_as_uint(magnitude * DOWN), drop = 23 - MANTISSA;
+        return (b + ((1u << (drop - 1)) - 1u) + ((b >> drop) & 1u)) >> drop;
+    }
+    static __device__ __forceinline__ float value(unsigned code) { return __uint_as_float(code << (23 - MANTISSA)) * UP; }
+};
+typedef Code<3, 7> MCode;
+typedef Code<4, 15> RCode;
+constexpr float M_TOP = 448.f, R_TOP = 1.9375f, SCALE_FLOOR = 0x1p-100f;
+
+__device__ __forceinline__ unsigned wave_max_bits(unsigned v)
+{
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v = max(v, (unsigned)__shfl_xor((int)v, o));
+    return v;
+}
+
+template <class T> __device__ __forceinline__ f32x4 load_upto4(const T *p, int n)
+{
+    if (n >= 4) return widened4<T>(load_pack<T, 4>(p));
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < 3; ++k) if (k < n) v[k] = (float)p[k];
+    return v;
+}
+template <class T> __device__ __forceinline__ void store_upto4(T *p, int n, f32x4 v)
+{
+    if (n >= 4) { store_pack<T, 4>(p, rounded4<T>(v)); return; }
+#pragma unroll
+    for (int k = 0; k < 3; ++k) if (k < n) p[k] = rounded<T>(v[k]);
+}
+__device__ __forceinline__ unsigned load_bytes(const uint8_t *p, int n)
+{
+    typedef unsigned loose __attribute__((aligned(1)));
+    if (n >= 4) return *reinterpret_cast<const loose *>(p);
+    unsigned v = 0;
+#pragma unroll
+    for (int k = 0; k < 3; ++k) if (k < n) v |= (unsigned)p[k] << (8 * k);
+    return v;
+}
+__device__ __forceinline__ void store_bytes(uint8_t *p, int n, unsigned v)
+{
+    typedef unsigned loose __attribute__((aligned(1)));
+    if (n >= 4) { *reinterpret_cast<loose *>(p) = v; return; }
+#pragma unroll
+    for (int k = 0; k < 3; ++k) if (k < n) p[k] = (uint8_t)(v >> (8 * k));
+}
+__device__ __forceinline__ float m_value(unsigned code, float scale)
+{
+    const float v = MCode::value(code & 127u) * scale;
+    return code & 128u ? -v : v;
+}
+
+template <class P, class G, int BITS>
+__global__ void __launch_bounds__(256) adamw_kernel(AdamwLaunch a)
+{
+    if (a.skip && a.skip[0] != 0.f) return;
+    const int k = find_tensor(a.first, a.count);
+    const ssm_adamw_tensor t = a.t[k];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const float gs = a.grad_scale ? a.grad_scale[0] : 1.f;
+    P *param = static_cast<P *>(t.param);
+    const G *grad = static_cast<const G *>(t.grad);
+#pragma unroll
+    for (int j = 0; j < ADAMW_CHUNK / (4 * SSM_ADAMW_BLOCK); ++j) {
+        const int64_t at = (int64_t)(blockIdx.x - a.first[k]) * ADAMW_CHUNK + (j * 4 + wave) * SSM_ADAMW_BLOCK + lane * 4;
+        const int64_t left = t.n - at;
+        const int n = left >= 4 ? 4 : left > 0 ? (int)left : 0;
+        const int64_t block = at / SSM_ADAMW_BLOCK;
+        const bool live = block * SSM_ADAMW_BLOCK < t.n;         // (uniform over the wavefront)
+        if (!live) break;
+        f32x4 p = load_upto4<P>(param + at, n), g = load_upto4<G>(grad + at, n), m, v;
+        if constexpr (BITS == 32) {
+            m = load_upto4<float>(static_cast<float *>(t.m) + at, n);
+            v = load_upto4<float>(static_cast<float *>(t.v) + at, n);
+        } else {
+            const unsigned mc = load_bytes(static_cast<uint8_t *>(t.m) + at, n), vc = load_bytes(static_cast<uint8_t *>(t.v) + at, n);
+            const float ms = t.m_scale[block], vs = t.v_scale[block];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                m[e] = m_value((mc >> (8 * e)) & 255u, ms);
+                const float r = RCode::value((vc >> (8 * e)) & 255u) * vs;
+                v[e] = r * r;
+            }
+        }
+        f32x4 root;
+        {
+#pragma clang fp contract(off)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float ge = g[e] * gs;
+                m[e] = m[e] * a.beta1 + ge * a.one_minus_beta1;
+                v[e] = v[e] * a.beta2 + (ge * ge) * a.one_minus_beta2;
+                root[e] = sqrtf(v[e]);
+                p[e] = p[e] * a.decay - a.rate * (m[e] / (root[e] / a.root2 + a.eps));
+            }
+        }
+        store_upto4<P>(param + at, n, p);
+        if constexpr (BITS == 32) {
+            store_upto4<float>(static_cast<float *>(t.m) + at, n, m);
+            store_upto4<float>(static_cast<float *>(t.v) + at, n, v);
+        } else {
+            // (as bit patterns: NaN is above infinity is above every number, so either reaches the scale)
+            unsigned mb = 0, rb = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                mb = max(mb, e < n ? __float_as_uint(fabsf(m[e])) : 0u);
+                rb = max(rb, e < n ? __float_as_uint(root[e]) & 0x7fffffffu : 0u);
+            }
+            const float mbig = __uint_as_float(wave_max_bits(mb)), rbig = __uint_as_float(wave_max_bits(rb));
+            const float mk = mbig < SCALE_FLOOR ? 0.f : mbig, rk = rbig < SCALE_FLOOR ? 0.f : rbig;
+            const float mi = mk == 0.f ? 0.f : M_TOP / mk, ri = rk == 0.f ? 0.f : R_TOP / rk;
+            unsigned mc = 0, vc = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const unsigned c = MCode::of(fabsf(m[e]) * mi) & 127u;
+                mc |= (c | (__float_as_uint(m[e]) >> 31) << 7) << (8 * e);
+                const float y = root[e] * ri;
+                vc |= (y > 0.f ? max(RCode::of(y), 1u) & 255u : 0u) << (8 * e);
+            }
+            store_bytes(static_cast<uint8_t *>(t.m) + at, n, mc);
+            store_bytes(static_cast<uint8_t *>(t.v) + at, n, vc);
+            if (lane == 0) { t.m_scale[block] = mk / M_TOP; t.v_scale[block] = rk / R_TOP; }
+        }
+    }
+}
+
+__global__ void __launch_bounds__(256) adamw_values_kernel(ValuesLaunch a)
+{
+    const int k = find_tensor(a.first, a.count);
+    const ssm_adamw_stored t = a.t[k];
+#pragma unroll
+    for (int j = 0; j < ADAMW_CHUNK / 1024; ++j) {
+        const int64_t at = (int64_t)(blockIdx.x - a.first[k]) * ADAMW_CHUNK + j * 1024 + threadIdx.x * 4;
+        const int64_t left = t.n - at, block = at / SSM_ADAMW_BLOCK;
+        if (left <= 0) break;
+        const int n = left >= 4 ? 4 : (int)left;
+        const unsigned mc = load_bytes(static_cast<const uint8_t *>(t.m) + at, n), vc = load_bytes(static_cast<const uint8_t *>(t.v) + at, n);
+        f32x4 m, v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            m[e] = m_value((mc >> (8 * e)) & 255u, t.m_scale[block]);
+            const float r = RCode::value((vc >> (8 * e)) & 255u) * t.v_scale[block];
+            v[e] = r * r;
+        }
+        if (t.m_out) store_upto4<float>(t.m_out + at, n, m);
+        if (t.v_out) store_upto4<float>(t.v_out + at, n, v);
+    }
+}
+
+// Launches `kernel(launch)` over all tensors, ADAMW_TENSORS at a time; empty ones take no place.
+template <class L, class D, class K> ssm_status launch_all(L &a, const D *tensors, int64_t count, hipStream_t s, K kernel)
+{
+    int64_t blocks = 0;
+    a.count = 0;
+    const auto flush = [&]() {
+        if (a.count == 0) return hipSuccess;
+        kernel(dim3((unsigned)blocks), a, s);
+        a.count = 0; blocks = 0;
+        return hipGetLastError();
+    };
+    for (int64_t i = 0; i < count; ++i) {
+        if (tensors[i].n == 0) continue;
+        const int64_t mine = (tensors[i].n + ADAMW_CHUNK - 1) / ADAMW_CHUNK;
+        if (a.count == ADAMW_TENSORS || blocks + mine > 0x7fffffffLL) { if (flush() != hipSuccess) return SSM_ERR_HIP; }
+        a.t[a.count] = tensors[i];
+        a.first[a.count++] = (unsigned)blocks;
+        blocks += mine;
+    }
+    return flush() == hipSuccess ? SSM_OK : SSM_ERR_HIP;
+}
+
+template <class P, class G, int BITS> ssm_status run_step(AdamwLaunch &a, const ssm_adamw_tensor *tensors, int64_t count, hipStream_t s)
+{
+    return launch_all(a, tensors, count, s, [](dim3 grid, const AdamwLaunch &l, hipStream_t st) {
+        hipLaunchKernelGGL((adamw_kernel<P, G, BITS>), grid, dim3(256), 0, st, l);
+    });
+}
+
+}  // namespace
+}  // namespace ssm
+
+using namespace ssm;
+
+extern "C" {
+
+ssm_status ssm_adamw_step(const ssm_adamw_tensor *tensors, int64_t count, ssm_adamw_rates r, int param_dtype, int grad_dtype,
+                          int state_bits, const float *grad_scale, const float *skip, void *stream)
+{
+    if (!tensors || count <= 0 || !dtype_known(param_dtype) || !dtype_known(grad_dtype) || (state_bits != 8 && state_bits != 32)) return SSM_ERR_INVALID_ARG;
+    if (param_dtype != SSM_F32 && param_dtype != grad_dtype) return SSM_ERR_INVALID_ARG;
+    if (!(r.beta1 >= 0. && r.beta1 < 1.) || !(r.beta2 >= 0. && r.beta2 < 1.) || !(r.eps >= 0.) || r.step < 1 || r.lr != r.lr || r.weight_decay != r.weight_decay)
+        return SSM_ERR_INVALID_ARG;
+    if (misaligned(grad_scale, 4) || misaligned(skip, 4)) return SSM_ERR_INVALID_ARG;
+    const size_t pb = dtype_bytes(param_dtype), gb = dtype_bytes(grad_dtype);
+    for (int64_t i = 0; i < count; ++i) {
+        const ssm_adamw_tensor &t = tensors[i];
+        if (t.n < 0) return SSM_ERR_INVALID_ARG;
+        if (t.n == 0) continue;
+        if (t.n > SSM_MAX_ELEMS) return SSM_ERR_UNSUPPORTED;
+        if (!t.param || !t.grad || !t.m || !t.v || misaligned(t.param, pb) || misaligned(t.grad, gb)) return SSM_ERR_INVALID_ARG;
+        if (state_bits == 32 ? misaligned(t.m, 4) || misaligned(t.v, 4)
+                             : !t.m_scale || !t.v_scale || misaligned(t.m_scale, 4) || misaligned(t.v_scale, 4))
+            return SSM_ERR_INVALID_ARG;
+    }
+    AdamwLaunch a{};
+    a.grad_scale = grad_scale; a.skip = skip;
+    a.decay = (float)(1. - r.lr * r.weight_decay);
+    a.beta1 = (float)r.beta1; a.beta2 = (float)r.beta2;
+    a.one_minus_beta1 = (float)(1. - r.beta1); a.one_minus_beta2 = (float)(1. - r.beta2);
+    a.rate = (float)(r.lr / (1. - std::pow(r.beta1, (double)r.step)));
+    a.root2 = (float)std::sqrt(1. - std::pow(r.beta2, (double)r.step));
+    a.eps = (float)r.eps;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return with_dtype(grad_dtype, [&](auto g) {
+        using G = decltype(g);
+        if (param_dtype == SSM_F32) return state_bits == 8 ? run_step<float, G, 8>(a, tensors, count, s) : run_step<float, G, 32>(a, tensors, count, s);
+        return state_bits == 8 ? run_step<G, G, 8>(a, tensors, count, s) : run_step<G, G, 32>(a, tensors, count, s);
+    });
+}
+
+ssm_status ssm_adamw_values(const ssm_adamw_stored *tensors, int64_t count, void *stream)
+{
+    if (!tensors || count <= 0) return SSM_ERR_INVALID_ARG;
+    for (int64_t i = 0; i < count; ++i) {
+        const ssm_adamw_stored &t = tensors[i];
+        if (t.n < 0) return SSM_ERR_INVALID_ARG;
+        if (t.n == 0) continue;
+        if (t.n > SSM_MAX_ELEMS) return SSM_ERR_UNSUPPORTED;
+        if (!t.m || !t.v || !t.m_scale || !t.v_scale || misaligned(t.m_scale, 4) || misaligned(t.v_scale, 4) || misaligned(t.m_out, 4) || misaligned(t.v_out, 4))
+            return SSM_ERR_INVALID_ARG;
+    }
+    ValuesLaunch a{};
+    return launch_all(a, tensors, count, static_cast<hipStream_t>(stream), [](dim3 grid, const ValuesLaunch &l, hipStream_t st) {
+        hipLaunchKernelGGL(adamw_values_kernel, grid, dim3(256), 0, st, l);
+    });
+}
+
+}  // extern "C"
