@@ -26,7 +26,7 @@ struct AdamwLaunch {
     unsigned first[ADAMW_TENSORS];           // first workgroup of every tensor
     int count;
     const float *grad_scale, *skip;
-    float decay, beta1, beta2, one_minus_beta1, one_minus_beta2, rate, root2, eps;
+    float decay, beta1, beta2, one_minus_beta1, one_minus_beta2, rate, inv_root2, eps;
 };
 struct ValuesLaunch {
     ssm_adamw_stored t[ADAMW_TENSORS];
@@ -139,7 +139,7 @@ __global__ void __launch_bounds__(256) adamw_kernel(AdamwLaunch a)
                 m[e] = m[e] * a.beta1 + ge * a.one_minus_beta1;
                 v[e] = v[e] * a.beta2 + (ge * ge) * a.one_minus_beta2;
                 root[e] = sqrtf(v[e]);
-                p[e] = p[e] * a.decay - a.rate * (m[e] / (root[e] / a.root2 + a.eps));
+                p[e] = p[e] * a.decay - a.rate * (m[e] / (root[e] * a.inv_root2 + a.eps));
             }
         }
         store_upto4<P>(param + at, n, p);
@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(256) adamw_kernel(AdamwLaunch a)
             }
             store_bytes(static_cast<uint8_t *>(t.m) + at, n, mc);
             store_bytes(static_cast<uint8_t *>(t.v) + at, n, vc);
-            if (lane == 0) { t.m_scale[block] = mk / M_TOP; t.v_scale[block] = rk / R_TOP; }
+            if (lane == 0) { t.m_scale[block] = mk * (1.f / M_TOP); t.v_scale[block] = rk * (1.f / R_TOP); }
         }
     }
 }
@@ -256,7 +256,7 @@ ssm_status ssm_adamw_step(const ssm_adamw_tensor *tensors, int64_t count, ssm_ad
     a.beta1 = (float)r.beta1; a.beta2 = (float)r.beta2;
     a.one_minus_beta1 = (float)(1. - r.beta1); a.one_minus_beta2 = (float)(1. - r.beta2);
     a.rate = (float)(r.lr / (1. - std::pow(r.beta1, (double)r.step)));
-    a.root2 = (float)std::sqrt(1. - std::pow(r.beta2, (double)r.step));
+    a.inv_root2 = 1.f / (float)std::sqrt(1. - std::pow(r.beta2, (double)r.step));
     a.eps = (float)r.eps;
     hipStream_t s = static_cast<hipStream_t>(stream);
     return with_dtype(grad_dtype, [&](auto g) {

@@ -7,13 +7,15 @@
 #include "elem.h"
 #include "ssm_internal.h"
 
+#include <type_traits>
+
 namespace ssm {
 namespace {
 
 constexpr size_t ALIGN = 256;
 inline bool misaligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
 
-constexpr float LOG2E = 1.44269504f, LN2 = 0.69314718f;
+constexpr float LOG2E = 1.44269504f;
 
 struct PolicyArgs {
     const void *logits; int64_t pitch;
@@ -25,24 +27,8 @@ struct PolicyArgs {
     const float *dloss;
     void *dlogits; int64_t dpitch;
     float *row_loss;                         // [N] weighted
+    float mean_weight;                       // of a row where none are given
 };
-
-// What the loss of a row is and its slope with respect to logp.
-struct RowTerms { float loss, slope; };
-__device__ __forceinline__ RowTerms row_terms(const PolicyArgs &a, int64_t n, float logp, float entropy)
-{
-    const float A = a.advantage[n], rho = expf(logp - a.logp_old[n]);
-    // (an advantage of zero makes the term zero, also where the ratio overflows)
-    const float raw = A == 0.f ? 0.f : rho * A, clipped = (rho < 1.f - a.terms.clip_low ? 1.f - a.terms.clip_low : rho > 1.f + a.terms.clip_high ? 1.f + a.terms.clip_high : rho) * A;
-    const bool held = clipped < raw;         // (a NaN is not held: it reaches the results)
-    RowTerms r = {-(held ? clipped : raw) - a.terms.entropy_coef * entropy, held ? 0.f : -raw};
-    if (a.logp_ref) {
-        const float d = a.logp_ref[n] - logp, e = expm1f(d);
-        r.loss += a.terms.kl_coef * (e - d);
-        r.slope -= a.terms.kl_coef * e;
-    }
-    return r;
-}
 
 __device__ __forceinline__ float wave_sum(float v)
 {
@@ -57,77 +43,302 @@ __device__ __forceinline__ float wave_max(float v)
     return v;
 }
 
-// One workgroup per row, three sweeps over it.
-template <class T, bool STATS, bool GRAD>
-__global__ void __launch_bounds__(256) policy_row_kernel(PolicyArgs a)
+// What is given per row, and what comes of it.  The few numbers of a row are computed in 64 bits: in 32 the logarithm of a large sum alone would put
+// a ratio off by 5e-7.
+struct Row {
+    int64_t action;
+    float old, advantage, ref, weight;
+    bool idle;
+};
+__device__ __forceinline__ Row load_row(const PolicyArgs &a, int64_t n)
 {
-    __shared__ float red[2][4];
-    const int64_t n = blockIdx.x;
-    const int tid = threadIdx.x, K = a.K, w = tid >> 6;
-    const T *x = static_cast<const T *>(a.logits) + n * a.pitch;
-    T *dx = GRAD ? static_cast<T *>(a.dlogits) + n * a.dpitch : nullptr;
-    const int64_t act = a.action[n];
-    const float weight = a.weight ? a.weight[n] : 1.f / (float)a.N;
-    bool idle = weight == 0.f || act < 0;
-    float lse = 0.f, entropy = 0.f, logp = 0.f, loss = 0.f, slope = 0.f;
-    float base = 0.f, off = 0.f;             // log p_k = (x_k - base) + off
-    if (!idle) {
-        if constexpr (STATS) {
-            const float xa = act < K ? (float)x[act] : NAN;      // (before the barriers: the gradient may be stored over the logits)
-            float m = -INFINITY;
-            for (int k = tid; k < K; k += 256) m = fmaxf(m, (float)x[k]);
-            m = wave_max(m);
-            if ((tid & 63) == 0) red[0][w] = m;
-            __syncthreads();
-            m = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
-            __syncthreads();
-            float s = 0.f, t = 0.f;
-            for (int k = tid; k < K; k += 256) {
-                const float d = (float)x[k] - m, e = __builtin_amdgcn_exp2f(d * LOG2E);
-                s += e;
-                t += e == 0.f ? 0.f : e * d;
-            }
-            s = wave_sum(s); t = wave_sum(t);
-            if ((tid & 63) == 0) { red[0][w] = s; red[1][w] = t; }
-            __syncthreads();
-            s = red[0][0] + red[0][1] + red[0][2] + red[0][3];
-            t = red[1][0] + red[1][1] + red[1][2] + red[1][3];
-            if (m == -INFINITY) {            // (uniform; a maximum passes over NaN)
-                bool nan = false;
-                for (int k = 0; k < K; ++k) nan |= x[k] != x[k];
-                idle = !nan;
-            }
-            const float ls = logf(s);
-            lse = m + ls; entropy = ls - t / s; logp = (xa - m) - ls;
-            base = m; off = -ls;
-        } else {
-            lse = a.lse[n]; entropy = a.entropy[n]; logp = a.logp[n];
-            idle = lse == -INFINITY;
-            const float xa = act < K ? (float)x[act] : NAN;
-            __syncthreads();
-            const bool taken = xa != -INFINITY;          // (else the action cannot be taken, and lse has to do)
-            base = taken ? xa : lse; off = taken ? logp : 0.f;
+    Row r;
+    r.action = a.action[n];
+    r.weight = a.weight ? a.weight[n] : a.mean_weight;
+    r.old = a.logp_old[n]; r.advantage = a.advantage[n];
+    r.ref = a.logp_ref ? a.logp_ref[n] : 0.f;
+    r.idle = r.weight == 0.f || r.action < 0;
+    return r;
+}
+struct Terms { double loss, slope; };        // of the row's loss, and of it with respect to logp
+__device__ __forceinline__ Terms row_terms(const PolicyArgs &a, const Row &r, double logp, double entropy)
+{
+    const double A = r.advantage, rho = exp(logp - (double)r.old), low = 1.0 - (double)a.terms.clip_low, high = 1.0 + (double)a.terms.clip_high;
+    // (an advantage of zero makes the term zero, also where the ratio overflows)
+    const double raw = A == 0.0 ? 0.0 : rho * A, clipped = (rho < low ? low : rho > high ? high : rho) * A;
+    const bool held = clipped < raw;         // (a NaN is not held: it reaches the results)
+    Terms t = {-(held ? clipped : raw) - (double)a.terms.entropy_coef * entropy, held ? 0.0 : -raw};
+    if (a.logp_ref) {
+        const double d = (double)r.ref - logp, e = expm1(d);
+        t.loss += (double)a.terms.kl_coef * (e - d);
+        t.slope -= (double)a.terms.kl_coef * e;
+    }
+    return t;
+}
+
+// Sums of a row (of a part of one): largest logit m, s = sum 2^d, t = sum 2^d d with d = (x - m) log2 e.  m starts at the lowest number, not at -infinity: a row with
+// no logit above -infinity ends with s = 0, and no difference of infinities is formed.  (A maximum passes over NaN; s does not.)
+constexpr float LOWEST = -3.402823466e38f, FAR = -1e4f;
+struct Sums { float m, s, t; };
+
+template <class T> struct Unit {             // 16 bytes of a row
+    static constexpr int V = 16 / sizeof(T);
+    typedef typename Pack<T, V>::type raw;
+    typedef float wide __attribute__((ext_vector_type(V)));
+};
+// unit from element k0 on; what lies past the end of the row is an action that cannot be taken
+template <class T> __device__ __forceinline__ typename Unit<T>::raw load_unit(const T *x, int k0, int K)
+{
+    constexpr int V = Unit<T>::V;
+    if (K - k0 >= V) return load_pack<T, V>(x + k0);
+    typename Unit<T>::raw v;
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = k0 + i < K ? x[k0 + i] : (T)-INFINITY;
+    return v;
+}
+template <class T> __device__ __forceinline__ void store_unit(T *x, int k0, int K, typename Unit<T>::wide g)
+{
+    constexpr int V = Unit<T>::V;
+    const typename Unit<T>::raw v = __builtin_convertvector(g, typename Unit<T>::raw);
+    if (K - k0 >= V) { store_pack<T, V>(x + k0, v); return; }
+#pragma unroll
+    for (int i = 0; i < V; ++i) if (k0 + i < K) x[k0 + i] = v[i];
+}
+template <class T> __device__ __forceinline__ typename Unit<T>::wide widen(typename Unit<T>::raw v) { return __builtin_convertvector(v, typename Unit<T>::wide); }
+
+// (16-bit units stay packed from one sweep over them to the next: widened ones would not fit the registers)
+template <class T, int U> __device__ __forceinline__ void stay_packed(typename Unit<T>::raw (&v)[U])
+{
+    typedef unsigned words __attribute__((ext_vector_type(4)));
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            words w = __builtin_bit_cast(words, v[j]);
+            asm volatile("" : "+v"(w));
+            v[j] = __builtin_bit_cast(typename Unit<T>::raw, w);
         }
     }
-    if (!idle) {
-        const RowTerms r = row_terms(a, n, logp, entropy);
-        loss = weight * r.loss; slope = weight * r.slope;
+}
+
+template <class T> __device__ __forceinline__ float max_of(typename Unit<T>::raw v, float m)
+{
+    const typename Unit<T>::wide x = widen<T>(v);
+#pragma unroll
+    for (int i = 0; i < Unit<T>::V; ++i) m = fmaxf(m, x[i]);
+    return m;
+}
+template <class T> __device__ __forceinline__ void add_unit(typename Unit<T>::raw v, float m, float &s, float &t)
+{
+    const typename Unit<T>::wide x = widen<T>(v);
+#pragma unroll
+    for (int i = 0; i < Unit<T>::V; ++i) {
+        const float d = (x[i] - m) * LOG2E, e = __builtin_amdgcn_exp2f(d);
+        s += e;
+        t = fmaf(e, fmaxf(d, FAR), t);       // (0 times -infinity is 0 here)
     }
-    if (STATS && tid == 0) {
-        a.row_loss[n] = idle ? 0.f : loss;
-        a.logp[n] = idle ? 0.f : logp; a.entropy[n] = idle ? 0.f : entropy; a.lse[n] = idle ? -INFINITY : lse;
+}
+
+// What the gradient of a row needs: log2 p_k = (x_k - base) log2 e + off,  a_k = p_k (c + eta log2 p_k) + [k = action] slope.
+struct Slope { float base, off, c, eta, slope; int action; bool idle; };
+template <class T> __device__ __forceinline__ typename Unit<T>::wide gradient(typename Unit<T>::raw v, int k0, const Slope &g)
+{
+    const typename Unit<T>::wide x = widen<T>(v);
+    typename Unit<T>::wide r;
+#pragma unroll
+    for (int i = 0; i < Unit<T>::V; ++i) {
+        const float lp = fmaf(x[i] - g.base, LOG2E, g.off), p = __builtin_amdgcn_exp2f(lp);
+        r[i] = p * fmaf(g.eta, fmaxf(lp, FAR), g.c);
+    }
+    if ((unsigned)(g.action - k0) < (unsigned)Unit<T>::V) {
+#pragma unroll
+        for (int i = 0; i < Unit<T>::V; ++i) r[i] += k0 + i == g.action ? g.slope : 0.f;
+    }
+    if (g.idle) {
+#pragma unroll
+        for (int i = 0; i < Unit<T>::V; ++i) r[i] = 0.f;
+    }
+    return r;
+}
+
+// The end of a row's statistics: its results (stored by one lane) and what its gradient needs.
+__device__ __forceinline__ Slope finish_row(const PolicyArgs &a, int64_t n, const Row &r, const Sums &q, float xa, bool store)
+{
+    const bool idle = r.idle || q.s == 0.f;
+    const double ls = log((double)q.s), entropy = ls - (double)q.t * 0.6931471805599453 / (double)q.s, logp = ((double)xa - (double)q.m) - ls;
+    const Terms t = row_terms(a, r, logp, entropy);
+    if (store) {
+        a.row_loss[n] = idle ? 0.f : (float)((double)r.weight * t.loss);
+        a.logp[n] = idle ? 0.f : (float)logp;
+        a.entropy[n] = idle ? 0.f : (float)entropy;
+        a.lse[n] = idle ? -INFINITY : (float)((double)q.m + ls);
+    }
+    const double w = (double)r.weight * (a.dloss ? (double)a.dloss[0] : 1.0), eta = w * (double)a.terms.entropy_coef, slope = w * t.slope;
+    return {q.m, (float)(-ls * 1.4426950408889634), (float)(eta * entropy - slope), (float)(eta * 0.6931471805599453), (float)slope, (int)r.action, idle};
+}
+// The same from what the forward pass stored.  (Differences from the logit of the action, not from lse: lse is rounded by 10^-3 at logits of 10^4.)
+__device__ __forceinline__ Slope stored_row(const PolicyArgs &a, int64_t n, const Row &r, float xa)
+{
+    const float lse = a.lse[n], logp = a.logp[n], entropy = a.entropy[n];
+    const Terms t = row_terms(a, r, logp, entropy);
+    const double w = (double)r.weight * (a.dloss ? (double)a.dloss[0] : 1.0), eta = w * (double)a.terms.entropy_coef, slope = w * t.slope;
+    const bool taken = xa != -INFINITY;      // (else the action cannot be taken and its logit is no reference)
+    return {taken ? xa : lse, taken ? logp * LOG2E : 0.f, (float)(eta * (double)entropy - slope), (float)(eta * 0.6931471805599453), (float)slope, (int)r.action,
+            r.idle || lse == -INFINITY};
+}
+template <class T> __device__ __forceinline__ float logit_of_action(const T *x, const Row &r, int K)
+{
+    return r.idle ? 0.f : r.action < K ? (float)x[r.action] : NAN;
+}
+
+// Short rows: 2^lanes neighbouring lanes hold a row, U units of 16 bytes each (U > 1: the whole wavefront), so a wavefront holds 64 >> lanes of them.
+template <class T, int U, bool STATS, bool GRAD>
+__global__ void __launch_bounds__(256) policy_wave_kernel(PolicyArgs a, int lanes)
+{
+    constexpr int V = Unit<T>::V;
+    const int lane = threadIdx.x & 63, width = 1 << lanes, sub = lane & (width - 1), K = a.K;
+    const int64_t want = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * (64 >> lanes) + (lane >> lanes), n = want < a.N ? want : a.N - 1;
+    const Row r = load_row(a, n);
+    const T *x = static_cast<const T *>(a.logits) + n * a.pitch;
+    const float xa = logit_of_action(x, r, K);
+    typename Unit<T>::raw v[U];
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[j][i] = (T)-INFINITY;
+    }
+    if (!r.idle) {
+#pragma unroll
+        for (int j = 0; j < U; ++j) v[j] = load_unit<T>(x, (sub + j * width) * V, K);
+    }
+    Slope g;
+    if constexpr (STATS) {
+        Sums q = {LOWEST, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < U; ++j) q.m = max_of<T>(v[j], q.m);
+        for (int o = 1; o < width; o <<= 1) q.m = fmaxf(q.m, __shfl_xor(q.m, o));
+        stay_packed<T>(v);
+#pragma unroll
+        for (int j = 0; j < U; ++j) add_unit<T>(v[j], q.m, q.s, q.t);
+        for (int o = 1; o < width; o <<= 1) { q.s += __shfl_xor(q.s, o); q.t += __shfl_xor(q.t, o); }
+        stay_packed<T>(v);
+        g = finish_row(a, n, r, q, xa, sub == 0 && want < a.N);
+    } else {
+        g = stored_row(a, n, r, xa);
     }
     if constexpr (GRAD) {
-        if (a.dloss) slope *= a.dloss[0];
-        const float eta = weight * a.terms.entropy_coef * (a.dloss ? a.dloss[0] : 1.f), c = eta * entropy - slope;
-        for (int k = tid; k < K; k += 256) {
-            float g = 0.f;
-            if (!idle) {
-                const float lp = ((float)x[k] - base) + off, p = __builtin_amdgcn_exp2f(lp * LOG2E);
-                g = p == 0.f ? 0.f : p * fmaf(eta, lp, c);
-                if (k == act) g += slope;
+        T *dx = static_cast<T *>(a.dlogits) + n * a.dpitch;
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            const int k0 = (sub + j * width) * V;
+            if (want < a.N && k0 < K) store_unit<T>(dx, k0, K, gradient<T>(v[j], k0, g));
+        }
+    }
+}
+
+struct RowLds { float m[16], s[16], t[16]; };
+// over all wavefronts of a workgroup; every thread gets the result
+__device__ __forceinline__ float row_max(RowLds &lds, float m, int waves)
+{
+    m = wave_max(m);
+    if ((threadIdx.x & 63) == 0) lds.m[threadIdx.x >> 6] = m;
+    __syncthreads();
+    m = lds.m[0];
+    for (int w = 1; w < waves; ++w) m = fmaxf(m, lds.m[w]);
+    return m;
+}
+__device__ __forceinline__ void row_sums(RowLds &lds, Sums &q, int waves)
+{
+    q.s = wave_sum(q.s); q.t = wave_sum(q.t);
+    if ((threadIdx.x & 63) == 0) { lds.s[threadIdx.x >> 6] = q.s; lds.t[threadIdx.x >> 6] = q.t; }
+    __syncthreads();
+    q.s = lds.s[0]; q.t = lds.t[0];
+    for (int w = 1; w < waves; ++w) { q.s += lds.s[w]; q.t += lds.t[w]; }
+}
+
+// Longer rows: a workgroup holds one in registers, U units of 16 bytes per thread, and reads it once.
+template <class T, int U, bool GRAD>
+__global__ void __launch_bounds__(1024) policy_row_kernel(PolicyArgs a)
+{
+    constexpr int V = Unit<T>::V;
+    __shared__ RowLds lds;
+    const int64_t n = blockIdx.x;
+    const int tid = threadIdx.x, threads = blockDim.x, waves = threads >> 6, K = a.K;
+    const Row r = load_row(a, n);
+    const T *x = static_cast<const T *>(a.logits) + n * a.pitch;
+    T *dx = GRAD ? static_cast<T *>(a.dlogits) + n * a.dpitch : nullptr;
+    typename Unit<T>::raw v[U];
+    Slope g;
+    if (r.idle) {                            // (uniform)
+        g = finish_row(a, n, r, Sums{0.f, 0.f, 0.f}, 0.f, tid == 0);
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[j][i] = (T)0.f;
+        }
+    } else {
+        const float xa = logit_of_action(x, r, K);
+#pragma unroll
+        for (int j = 0; j < U; ++j) v[j] = load_unit<T>(x, (tid + j * threads) * V, K);
+        Sums q = {LOWEST, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < U; ++j) q.m = max_of<T>(v[j], q.m);
+        q.m = row_max(lds, q.m, waves);
+        stay_packed<T>(v);
+#pragma unroll
+        for (int j = 0; j < U; ++j) add_unit<T>(v[j], q.m, q.s, q.t);
+        stay_packed<T>(v);
+        row_sums(lds, q, waves);             // (behind its barrier the gradient may be stored over the logits)
+        g = finish_row(a, n, r, q, xa, tid == 0);
+    }
+    if constexpr (GRAD) {
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            const int k0 = (tid + j * threads) * V;
+            if (k0 < K) store_unit<T>(dx, k0, K, gradient<T>(v[j], k0, g));
+        }
+    }
+}
+
+// Rows that no workgroup's registers hold, and the gradient from stored statistics, which needs nothing held: the row is read for either part.
+template <class T, bool STATS, bool GRAD>
+__global__ void __launch_bounds__(1024) policy_stream_kernel(PolicyArgs a)
+{
+    constexpr int V = Unit<T>::V;
+    __shared__ RowLds lds;
+    const int64_t n = blockIdx.x;
+    const int tid = threadIdx.x, threads = blockDim.x, waves = threads >> 6, K = a.K, stride = threads * V;
+    const Row r = load_row(a, n);
+    const T *x = static_cast<const T *>(a.logits) + n * a.pitch;
+    const float xa = logit_of_action(x, r, K);
+    Slope g;
+    if constexpr (STATS) {
+        Sums q = {LOWEST, 0.f, 0.f};
+        if (!r.idle) {                       // (uniform)
+            for (int k0 = tid * V; k0 < K; k0 += stride) {
+                const typename Unit<T>::raw v = load_unit<T>(x, k0, K);
+                const float m = max_of<T>(v, q.m), d = fmaxf((q.m - m) * LOG2E, FAR), scale = __builtin_amdgcn_exp2f(d);
+                q.t = scale * fmaf(q.s, d, q.t);
+                q.s *= scale;
+                q.m = m;
+                add_unit<T>(v, m, q.s, q.t);
             }
-            dx[k] = rounded<T>(g);
+            const float m = row_max(lds, q.m, waves), d = fmaxf((q.m - m) * LOG2E, FAR), scale = __builtin_amdgcn_exp2f(d);
+            q = {m, q.s * scale, scale * fmaf(q.s, d, q.t)};
+            row_sums(lds, q, waves);
+        }
+        g = finish_row(a, n, r, q, xa, tid == 0);
+    } else {
+        __syncthreads();                     // every thread has read the action's logit before the first one stores over it
+        g = stored_row(a, n, r, xa);
+    }
+    if constexpr (GRAD) {
+        T *dx = static_cast<T *>(a.dlogits) + n * a.dpitch;
+        for (int k0 = tid * V; k0 < K; k0 += stride) {
+            typename Unit<T>::raw v;
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] = (T)0.f;
+            if (!g.idle) v = load_unit<T>(x, k0, K);
+            store_unit<T>(dx, k0, K, gradient<T>(v, k0, g));
         }
     }
 }
@@ -172,9 +383,38 @@ ssm_status launch_sum(const PolicyArgs &a, float *loss, hipStream_t s)
     hipLaunchKernelGGL(policy_sum_kernel, dim3(1), dim3(1024), 0, s, a.row_loss, a.N, loss);
     return hipGetLastError() == hipSuccess ? SSM_OK : SSM_ERR_HIP;
 }
+// Who holds a row: part of a wavefront, a wavefront, a workgroup, or nobody.
+template <class T, bool STATS, bool GRAD> void launch_rows_of(const PolicyArgs &a, hipStream_t s)
+{
+    constexpr int V = Unit<T>::V;
+    const int64_t units = ((int64_t)a.K + V - 1) / V;
+    const auto wave = [&](auto u, int lanes) {
+        const int64_t rows = 4 * (64 >> lanes);
+        hipLaunchKernelGGL((policy_wave_kernel<T, decltype(u)::value, STATS, GRAD>), dim3((unsigned)((a.N + rows - 1) / rows)), dim3(256), 0, s, a, lanes);
+    };
+    if (units <= 64) {
+        int lanes = 0;
+        while ((1 << lanes) < units) ++lanes;
+        return wave(std::integral_constant<int, 1>{}, lanes);
+    }
+    if (units <= 128) return wave(std::integral_constant<int, 2>{}, 6);
+    if (units <= 256) return wave(std::integral_constant<int, 4>{}, 6);
+    if (units <= 512) return wave(std::integral_constant<int, 8>{}, 6);
+    if constexpr (STATS) {
+        const auto row = [&](auto u, int threads) {
+            hipLaunchKernelGGL((policy_row_kernel<T, decltype(u)::value, GRAD>), dim3((unsigned)a.N), dim3(threads), 0, s, a);
+        };
+        if (units <= 256 * 4) return row(std::integral_constant<int, 4>{}, 256);
+        if (units <= 256 * 8) return row(std::integral_constant<int, 8>{}, 256);
+        if (units <= 512 * 8) return row(std::integral_constant<int, 8>{}, 512);
+        if (units <= 512 * 16) return row(std::integral_constant<int, 16>{}, 512);
+        if (units <= 1024 * 16) return row(std::integral_constant<int, 16>{}, 1024);
+    }
+    hipLaunchKernelGGL((policy_stream_kernel<T, STATS, GRAD>), dim3((unsigned)a.N), dim3(units <= 2048 ? 256 : 1024), 0, s, a);
+}
 template <bool STATS, bool GRAD> ssm_status launch_rows(const PolicyArgs &a, int dtype, hipStream_t s)
 {
-    with_dtype(dtype, [&](auto t) { hipLaunchKernelGGL((policy_row_kernel<decltype(t), STATS, GRAD>), dim3((unsigned)a.N), dim3(256), 0, s, a); });
+    with_dtype(dtype, [&](auto t) { launch_rows_of<decltype(t), STATS, GRAD>(a, s); });
     return hipGetLastError() == hipSuccess ? SSM_OK : SSM_ERR_HIP;
 }
 
@@ -197,7 +437,7 @@ ssm_status ssm_policy_loss_fwd(const void *logits, int64_t pitch, const int64_t 
                                void *workspace, size_t ws_bytes, void *stream)
 {
     PolicyArgs a{logits, pitch, action, logp_old, advantage, weight, logp_ref, terms, N, (int)K, logp, entropy, lse, nullptr, nullptr, 0,
-                 static_cast<float *>(workspace)};
+                 static_cast<float *>(workspace), N > 0 ? 1.f / (float)N : 0.f};
     if (const ssm_status rc = check_policy(a, dtype, N, K)) return rc;
     if (!loss || misaligned(loss, 4)) return SSM_ERR_INVALID_ARG;
     if (!workspace || misaligned(workspace, ALIGN) || ws_bytes < ssm_policy_loss_workspace_bytes(N, K)) return SSM_ERR_WORKSPACE;
@@ -212,7 +452,7 @@ ssm_status ssm_policy_loss_bwd(const void *logits, int64_t pitch, const int64_t 
                                const float *dloss, void *dlogits, int64_t dpitch, void *stream)
 {
     PolicyArgs a{logits, pitch, action, logp_old, advantage, weight, logp_ref, terms, N, (int)K, const_cast<float *>(logp),
-                 const_cast<float *>(entropy), const_cast<float *>(lse), dloss, dlogits, dpitch, nullptr};
+                 const_cast<float *>(entropy), const_cast<float *>(lse), dloss, dlogits, dpitch, nullptr, N > 0 ? 1.f / (float)N : 0.f};
     if (const ssm_status rc = check_policy(a, dtype, N, K)) return rc;
     if (const ssm_status rc = check_gradient(a, dtype, N, K)) return rc;
     return launch_rows<false, true>(a, dtype, static_cast<hipStream_t>(stream));
@@ -224,7 +464,7 @@ ssm_status ssm_policy_loss_grad(const void *logits, int64_t pitch, const int64_t
                                 float *lse, void *dlogits, int64_t dpitch, void *workspace, size_t ws_bytes, void *stream)
 {
     PolicyArgs a{logits, pitch, action, logp_old, advantage, weight, logp_ref, terms, N, (int)K, logp, entropy, lse, dloss, dlogits, dpitch,
-                 static_cast<float *>(workspace)};
+                 static_cast<float *>(workspace), N > 0 ? 1.f / (float)N : 0.f};
     if (const ssm_status rc = check_policy(a, dtype, N, K)) return rc;
     if (const ssm_status rc = check_gradient(a, dtype, N, K)) return rc;
     if (!loss || misaligned(loss, 4)) return SSM_ERR_INVALID_ARG;
