@@ -1,6 +1,6 @@
 """Builds libssmscan.so (HIP, gfx950 only) in-tree with hipcc: one object per source, compiled in
-parallel, then one link.  Beside it _ssmbind.so, the native half of the Python binding (host code only, against
-torch's C++ headers), which is linked to the library."""
+parallel, then one link.  Beside it _ssmbind.so and _ssmlearn.so, the native halves of the Python binding (host code only,
+against torch's C++ headers), which are linked to the library."""
 from __future__ import annotations
 
 import concurrent.futures
@@ -15,10 +15,12 @@ OBJDIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libssmscan.so")
 BIND = os.path.join(HERE, "_ssmbind.so")
 BIND_SOURCE = os.path.join(CSRC, "pybind.cpp")
+BIND_LEARN = os.path.join(HERE, "_ssmlearn.so")
+BINDS = {BIND: BIND_SOURCE, BIND_LEARN: os.path.join(CSRC, "pybind_learn.cpp")}
 SOURCES = ["products2.hip", "products3.hip", "params.hip", "block.hip", "narrow.hip", "scan.hip", "ssm_api.hip", "gemm.hip", "noalloc.hip",
            "gated.hip", "policy.hip", "adamw.hip"]
 HEADERS = [os.path.join(CSRC, h) for h in ("ssm_internal.h", "fast_div.h", "store_rule.h", "gemm_common.h", "gemm_kernel.h", "gemm_packed.h", "pk_units.h", "pack.h", "lookback.h",
-                                             "elem.h")] + \
+                                             "elem.h", "pybind_common.h")] + \
           [os.path.join(os.path.dirname(HERE), "include", h) for h in ("ssm.h", "ssm_measure.h", "ssm_learn.h")]
 # packed-fp32 instructions are switched off on purpose (target feature removed for device code)
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -31,12 +33,12 @@ def _newest_header() -> float:
 
 
 def is_stale() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(BIND):
+    if not os.path.exists(LIB) or not all(os.path.exists(b) for b in BINDS):
         return True
     t = os.path.getmtime(LIB)
     deps = [os.path.join(CSRC, s) for s in SOURCES] + HEADERS
-    return any(os.path.getmtime(d) > t for d in deps) or any(os.path.getmtime(d) > os.path.getmtime(BIND)
-                                                             for d in [BIND_SOURCE] + HEADERS)
+    return any(os.path.getmtime(d) > t for d in deps) or any(os.path.getmtime(d) > os.path.getmtime(bind)
+                                                             for bind, src in BINDS.items() for d in [src] + HEADERS)
 
 
 def _compile(hipcc: str, src: str, obj: str, verbose: bool) -> None:
@@ -46,15 +48,24 @@ def _compile(hipcc: str, src: str, obj: str, verbose: bool) -> None:
     subprocess.check_call(cmd)
 
 
-def _bind_command(out: str):
-    """The host compiler's command for the native half of the binding (torch is located, not imported)."""
+def _bind_command(out: str, source: str = BIND_SOURCE):
+    """The host compiler's command for a native half of the binding (torch is located, not imported)."""
     torch_dir = os.path.dirname(importlib.util.find_spec("torch").origin)
     inc, lib = os.path.join(torch_dir, "include"), os.path.join(torch_dir, "lib")
     return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden", "-w",
             "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1", "-I" + inc, "-I" + os.path.join(inc, "torch", "csrc", "api", "include"),
-            "-I" + sysconfig.get_paths()["include"], "-I/opt/rocm/include", BIND_SOURCE, "-o", out,
+            "-I" + sysconfig.get_paths()["include"], "-I/opt/rocm/include", source, "-o", out,
             "-L" + HERE, "-lssmscan", "-L" + lib, "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_hip", "-ltorch_python",
             "-Wl,-rpath,$ORIGIN"]
+
+
+def _build_bind(out: str, source: str, verbose: bool) -> None:
+    tmp = out + ".tmp%d" % os.getpid()
+    cmd = _bind_command(tmp, source)
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    subprocess.check_call(cmd)
+    os.replace(tmp, out)
 
 
 def build(force: bool = True, verbose: bool = False) -> str:
@@ -83,13 +94,12 @@ def build(force: bool = True, verbose: bool = False) -> str:
         print(" ".join(cmd), flush=True)
     subprocess.check_call(cmd)
     os.replace(tmp, LIB)
-    if force or not os.path.exists(BIND) or os.path.getmtime(BIND) < max(os.path.getmtime(BIND_SOURCE), hdr_t):
-        tmp = BIND + ".tmp%d" % os.getpid()
-        cmd = _bind_command(tmp)
-        if verbose:
-            print(" ".join(cmd), flush=True)
-        subprocess.check_call(cmd)
-        os.replace(tmp, BIND)
+    stale = [(bind, src) for bind, src in BINDS.items()
+             if force or not os.path.exists(bind) or os.path.getmtime(bind) < max(os.path.getmtime(src), hdr_t)]
+    if stale:
+        with concurrent.futures.ThreadPoolExecutor(max_workers=len(stale)) as pool:
+            for f in [pool.submit(_build_bind, bind, src, verbose) for bind, src in stale]:
+                f.result()
     return LIB
 
 

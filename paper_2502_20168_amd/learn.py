@@ -9,8 +9,8 @@ from __future__ import annotations
 import ctypes
 from typing import Dict, List, Optional, Sequence, Tuple
 
-from .binding import (SSM_ERR_INVALID_ARG, SSM_ERR_UNSUPPORTED, SSM_ERR_WORKSPACE, SSM_OK, SsmError, _chk, _own_workspace, _ptr, _stream, _torch, lib,
-                      ssm_workspace_status)
+from .binding import (SSM_ERR_INVALID_ARG, SSM_ERR_UNSUPPORTED, SSM_ERR_WORKSPACE, SSM_OK, SsmError, _chk, _done, _GeneralPathOnly, _handle, _own_workspace,
+                      _ptr, _stream, _torch, lib, ssm_workspace_status)
 
 __all__ = ["ssm_gated_carry_rows", "ssm_gated_workspace_bytes", "ssm_gated_scan_fwd", "ssm_gated_scan_bwd", "ssm_gated_step",
            "ssm_policy_loss_workspace_bytes", "ssm_policy_loss_fwd", "ssm_policy_loss_bwd", "ssm_policy_loss_grad",
@@ -48,6 +48,23 @@ class _AdamwRates(ctypes.Structure):
 
 
 _ready = None
+_native = None
+
+
+def _bind():
+    """The native half (csrc/pybind_learn.cpp): it answers None for what it does not take, and the general path below follows."""
+    global _native
+    if _native is None:
+        _lib()
+        try:
+            from . import _ssmlearn
+            _native = _ssmlearn
+        except ImportError as e:
+            import warnings
+            warnings.warn("the native half of the binding does not load (%s): run `python paper_2502_20168_amd/build.py`; calls go "
+                          "through ctypes" % e, RuntimeWarning, stacklevel=3)
+            _native = _GeneralPathOnly()
+    return _native
 
 
 def _lib():
@@ -148,6 +165,9 @@ def ssm_gated_scan_fwd(gate, u, is_first=None, h0=None, *, linear: bool = False,
                        out: Optional[Dict] = None) -> Dict[str, object]:
     """h_t = [not first_t] f_t h_{t-1} + (1 - f_t) u_t with f = sigmoid(gate); linear: [not first_t] gate_t h_{t-1} + u_t.
     gate, u [Bt,L,D].  Returns dict(h [Bt,L,D], h_last [Bt,D] float32, carry for the gradient pass or None)."""
+    r = (_native or _bind()).gated_scan_fwd(gate, u, is_first, h0, linear, want_carry, workspace, _handle(stream), out)
+    if r is not None:
+        return _done(r, "ssm_gated_scan_fwd")
     torch = _torch()
     Bt, L, D, code = _check_gated(gate, u, is_first, h0)
     rows = ssm_gated_carry_rows(L)
@@ -167,6 +187,9 @@ def ssm_gated_scan_bwd(gate, u, is_first, h0, carry, dh, dh_last=None, *, linear
                        stream=None, out: Optional[Dict] = None) -> Dict[str, object]:
     """Gradient pass of ssm_gated_scan_fwd (carry: its result) for sum(dh h) + sum(dh_last h_last).
     Returns dict(dgate, du [Bt,L,D], dh0 [Bt,D] float32 or None)."""
+    r = (_native or _bind()).gated_scan_bwd(gate, u, is_first, h0, carry, dh, dh_last, linear, want_dh0, workspace, _handle(stream), out)
+    if r is not None:
+        return _done(r, "ssm_gated_scan_bwd")
     torch = _torch()
     Bt, L, D, code = _check_gated(gate, u, is_first, h0)
     rows = ssm_gated_carry_rows(L)
@@ -190,6 +213,9 @@ def ssm_gated_scan_bwd(gate, u, is_first, h0, carry, dh, dh_last=None, *, linear
 def ssm_gated_step(gate, u, h_prev=None, is_first=None, *, linear: bool = False, h=None, y=None, stream=None):
     """One step of Bt sequences: gate, u [Bt,D], h_prev [Bt,D] float32 or None.  Returns (y, h): the new state in the type of u and
     in float32 (h may be h_prev, which is then updated in place)."""
+    r = (_native or _bind()).gated_step(gate, u, h_prev, is_first, linear, h, y, _handle(stream))
+    if r is not None:
+        return _done(r, "ssm_gated_step")
     torch = _torch()
     if gate.dim() != 2:
         raise ValueError("gate must be [Bt,D]")
@@ -255,6 +281,10 @@ def _check_dlogits(logits, dlogits, out):
 def ssm_policy_loss_fwd(logits, action, logp_old, advantage, weight=None, logp_ref=None, *, clip_low: float = 0.2, clip_high: float = 0.2,
                         kl_coef: float = 0.0, entropy_coef: float = 0.0, workspace=None, stream=None, out: Optional[Dict] = None) -> Dict[str, object]:
     """Clipped policy loss of N rows of logits [N,K].  Returns dict(loss [], logp, entropy, lse [N]), float32."""
+    r = (_native or _bind()).policy_loss_fwd(logits, action, logp_old, advantage, weight, logp_ref, clip_low, clip_high, kl_coef, entropy_coef,
+                                             workspace, _handle(stream), out)
+    if r is not None:
+        return _done(r, "ssm_policy_loss_fwd")
     N, K, code = _check_policy(logits, action, logp_old, advantage, weight, logp_ref)
     r = _policy_outputs(logits, out)
     ws = _policy_workspace(workspace, N, K, logits.device, stream)
@@ -268,6 +298,10 @@ def ssm_policy_loss_bwd(logits, action, logp_old, advantage, weight, logp_ref, l
                         clip_high: float = 0.2, kl_coef: float = 0.0, entropy_coef: float = 0.0, dlogits=None, stream=None):
     """Gradient with respect to the logits, from the forward call's logp, entropy and lse; dloss: float32 scalar tensor or None for 1.
     Returns dlogits [N,K] in the type of the logits (`dlogits=logits` stores it over them)."""
+    r = (_native or _bind()).policy_loss_bwd(logits, action, logp_old, advantage, weight, logp_ref, clip_low, clip_high, kl_coef, entropy_coef,
+                                             logp, entropy, lse, dloss, dlogits, _handle(stream))
+    if r is not None:
+        return _done(r, "ssm_policy_loss_bwd")
     torch = _torch()
     N, K, code = _check_policy(logits, action, logp_old, advantage, weight, logp_ref)
     for name, t in (("logp", logp), ("entropy", entropy), ("lse", lse)):
@@ -284,6 +318,10 @@ def ssm_policy_loss_grad(logits, action, logp_old, advantage, weight=None, logp_
                          clip_high: float = 0.2, kl_coef: float = 0.0, entropy_coef: float = 0.0, workspace=None, stream=None,
                          out: Optional[Dict] = None) -> Dict[str, object]:
     """Loss and gradient in one call: dict(loss, logp, entropy, lse, dlogits); out={"dlogits": logits} stores it over the logits."""
+    r = (_native or _bind()).policy_loss_grad(logits, action, logp_old, advantage, weight, logp_ref, clip_low, clip_high, kl_coef, entropy_coef,
+                                              dloss, workspace, _handle(stream), out)
+    if r is not None:
+        return _done(r, "ssm_policy_loss_grad")
     torch = _torch()
     N, K, code = _check_policy(logits, action, logp_old, advantage, weight, logp_ref)
     _chk(dloss, torch.float32, () if dloss is None else tuple(dloss.shape) if dloss.numel() == 1 else (), "dloss")
@@ -328,6 +366,11 @@ def ssm_adamw_step(params: Sequence, grads: Sequence, m: Sequence, v: Sequence, 
     """One AdamW step over all tensors at once, in place.  params and grads: lists of contiguous tensors, each list of one type;
     m, v (and, where they are bytes, m_scale, v_scale) as ssm_adamw_state makes them; step counts from 1.  grad_scale and skip:
     float32 tensors of one element, read on the device: gradients are multiplied by the first, and nothing changes where the second is not zero."""
+    r = (_native or _bind()).adamw_step(params, grads, m, v, m_scale, v_scale, lr, beta1, beta2, eps, weight_decay, step, grad_scale, skip,
+                                        _handle(stream))
+    if r is not None:
+        _done(r, "ssm_adamw_step")
+        return
     torch = _torch()
     if len(params) == 0:
         raise ValueError("params must hold at least one tensor")
@@ -364,6 +407,10 @@ def ssm_adamw_values(m: Sequence, v: Sequence, m_scale: Sequence, v_scale: Seque
         raise ValueError("m must hold at least one tensor")
     m_out = [torch.empty(t.shape, dtype=torch.float32, device=t.device) for t in m] if m_out is None else m_out
     v_out = [torch.empty(t.shape, dtype=torch.float32, device=t.device) for t in m] if v_out is None else v_out
+    r = (_native or _bind()).adamw_values(m, v, m_scale, v_scale, m_out, v_out, _handle(stream))
+    if r is not None:
+        _done(r, "ssm_adamw_values")
+        return m_out, v_out
     _same_length(m, v=v, m_scale=m_scale, v_scale=v_scale, m_out=m_out, v_out=v_out)
     rows = (_AdamwStored * len(m))()
     for i, t in enumerate(m):
