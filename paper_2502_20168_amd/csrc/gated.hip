@@ -10,6 +10,8 @@
 #include "lookback.h"
 #include "ssm_internal.h"
 
+#include <type_traits>
+
 namespace ssm {
 namespace {
 
@@ -29,9 +31,16 @@ struct GatedArgs {
     ssm_strides hs, dgs, dus;
     float *h_last, *carry, *dh0;
     int Bt, L, D;
-    int lgcx, lgtr;                          // log2 of a workgroup's vectors of channels and of the threads along time of one sequence
+    int lgcx, lgspan;                        // log2 of a workgroup's vectors of channels and of the lanes of a wavefront that hold one sequence
+    int rows, seqs;                          // threads along time of a sequence, sequences of a workgroup (several: each within a wavefront)
     int nCX, nTB, carry_rows;                // channel blocks, chunks along time
+    // chunks in workgroups of their own
+    unsigned long long *desc;                // [nTB][nCX * Bt][3][64] tagged words, zero on entry: A, S and the state behind the chunk
+    uint32_t *ticket, *err;
+    uint32_t spin_limit;
+    FastDiv by_chains;                       // nCX * Bt
 };
+constexpr int GATED_DESC_WORDS = 3 * 64;
 
 // sigmoid(z) and 1 - sigmoid(z), both to the relative precision of the exponential: the difference where it is at least a half, exp(-z) sigmoid(z) else.
 struct Gate { float f, i; };
@@ -107,52 +116,137 @@ __device__ __forceinline__ Map get(const MapLds &s, int w, int c) { return {s.A[
 // What a thread owns: GE steps of GV channels of one sequence.  Threads past the end of an axis take the last valid place and store nothing.
 // The last vector of a row is moved back so that it ends with the row: its channels are computed twice, with the same operations, and the same values stored twice.
 struct Place {
-    int vec, row, seq, ch, lane, span, wave, wave0, waves;      // wave: of the workgroup; wave0, waves: the first and the number of those that hold this sequence
+    int vec, row, seq, ch, lane, span, wave, waves;      // waves: of a sequence, where there is one per workgroup
     bool stored;
-    __device__ __forceinline__ Place(const GatedArgs &a)
+    __device__ __forceinline__ Place(const GatedArgs &a, int chain)
     {
-        const int tid = threadIdx.x, cx = 1 << a.lgcx, tr = 1 << a.lgtr;
+        const int tid = threadIdx.x, cx = 1 << a.lgcx;
+        const bool several = a.seqs > 1;
         lane = tid & 63;
+        wave = tid >> 6;
+        span = 1 << a.lgspan;
         vec = tid & (cx - 1);
-        row = (tid >> a.lgcx) & (tr - 1);
-        const int s = tid >> (a.lgcx + a.lgtr), seqs = (int)blockDim.x >> (a.lgcx + a.lgtr);
-        const int blk = (int)blockIdx.x, sb = blk / a.nCX, cb = blk - sb * a.nCX;
-        const int b = sb * seqs + s, v = cb * cx + vec;
+        row = (several ? tid & (span - 1) : tid) >> a.lgcx;
+        waves = several ? 1 : (int)blockDim.x >> 6;
+        const int s = several ? tid >> a.lgspan : 0, sb = chain / a.nCX, cb = chain - sb * a.nCX;
+        const int b = sb * a.seqs + s, v = cb * cx + vec;
         stored = b < a.Bt && v * GV < a.D;
         seq = min(b, a.Bt - 1);
         ch = max(0, min(v * GV, a.D - GV));
-        span = min(64, cx * tr);
-        waves = max(1, (cx * tr) >> 6);
-        wave = tid >> 6;
-        wave0 = wave & ~(waves - 1);
     }
 };
 
-// (D < GV: one vector, its missing channels repeat the last one)
-template <class T> __device__ __forceinline__ typename Pack<T, 4>::type load_channels(const T *p, int D)
+// What a chunk's neighbours hand over where every chunk has a workgroup of its own.  A workgroup publishes the map of its chunk before it waits for anything; then
+// each of its rows fetches the map of one earlier chunk of its group of `rows` chunks, all at once, and one row the state behind the last chunk of
+// the group before.  The order of the compositions is fixed, whatever the timing: results are repeatable.  Chunks are numbered by a ticket per chain (the chunks of one
+// sequence and channel block), so that a workgroup waits for such as have started; a wait that gives up hands on NaN and says so in the workspace.
+__device__ __forceinline__ bool wait_words(const unsigned long long *w, unsigned limit, f32x4 &v, unsigned &tag)
 {
-    if (D >= GV) return load_pack<T, 4>(p);
+    for (unsigned spins = 0;; ++spins) {
+        unsigned long long q[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) q[k] = poll_word(w + k);
+        bool all = true;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) { all = all && word_tag(q[k]) != 0; v[k] = word_value(q[k]); }
+        tag = word_tag(q[0]);
+        if (all) return true;
+        if (spins >= limit) return false;
+        __builtin_amdgcn_s_sleep(2);
+    }
+}
+__device__ __forceinline__ void publish4(unsigned long long *w, f32x4 v, unsigned tag)
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k) publish_word(w + k, v[k], tag);
+}
+// UP: rows in the order of time.  `chunk`: number along the direction of the scan; `total`: the chunk's map, valid where `ends`; v0: what flows into the first chunk.
+template <bool UP> __device__ __forceinline__ f32x4 look_back(const GatedArgs &a, const Place &p, MapLds &lds, f32x4 *s_base, int chunk, int chain, const Map &total, bool ends, f32x4 v0)
+{
+    const int cx = 1 << a.lgcx, chains = a.nCX * a.Bt, group = chunk / a.rows * a.rows, row = UP ? p.row : a.rows - 1 - p.row;
+    unsigned long long *mine = a.desc + ((int64_t)chunk * chains + chain) * GATED_DESC_WORDS + p.vec * GV;
+    const int64_t back = (int64_t)chains * GATED_DESC_WORDS;
+    if (ends && chunk + 1 < a.nTB) {
+        publish4(mine, total.A, 1);
+        publish4(mine + 64, total.S, total.r ? 2 : 1);
+    }
+    f32x4 v = v0;
+    if (chunk > 0) {                         // (uniform)
+        const f32x4 nan = {__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
+        Map m = identity();
+        if (group + row < chunk) {
+            const unsigned long long *w = mine - (chunk - group - row) * back;
+            unsigned tag;
+            const bool got = wait_words(w, a.spin_limit, m.A, tag) && wait_words(w + 64, a.spin_limit, m.S, tag);
+            m.r = tag == 2;
+            if (!got) { atomicOr(a.err, 1u); m.S = nan; m.r = 1; }
+        }
+        if (group > 0 && row == 0) {
+            unsigned tag;
+            f32x4 base;
+            if (!wait_words(mine - (chunk - group + 1) * back + 128, a.spin_limit, base, tag)) { atomicOr(a.err, 1u); base = nan; }
+            s_base[p.vec] = base;
+        }
+        m = inclusive_in_wave<UP>(m, p.lane, cx, p.span);
+        __syncthreads();                     // (the maps of the chunk itself have been read)
+        if (UP ? p.lane >= 64 - cx : p.lane < cx) put(lds, p.wave, p.vec, m);
+        __syncthreads();
+        Map w = identity();
+        for (int k = 0; k < p.waves; ++k) w = after(get(lds, UP ? k : p.waves - 1 - k, p.vec), w);
+        v = apply(w, group > 0 ? s_base[p.vec] : v0);
+    }
+    if (ends && chunk + 1 < a.nTB && (chunk + 1) % a.rows == 0) publish4(mine + 128, apply(total, v), 3);
+    return v;
+}
+// the chunk and the chain of this workgroup
+__device__ __forceinline__ int take_ticket(const GatedArgs &a, int &chain)
+{
+    __shared__ int s_chunk;
+    const int chains = a.nCX * a.Bt;
+    chain = (int)blockIdx.x - (int)a.by_chains(blockIdx.x) * chains;
+    if (threadIdx.x == 0) s_chunk = (int)atomicAdd(a.ticket + (int64_t)chain * SCAN_TICKET_STRIDE, 1u);
+    __syncthreads();
+    return __builtin_amdgcn_readfirstlane(s_chunk);
+}
+
+// NARROW: rows of fewer than GV channels, whose one vector repeats the last of them.
+template <class T, bool NARROW> __device__ __forceinline__ typename Pack<T, 4>::type load_channels(const T *p, int D)
+{
+    if constexpr (!NARROW) return load_pack<T, 4>(p);
     typename Pack<T, 4>::type v;
 #pragma unroll
     for (int k = 0; k < GV; ++k) v[k] = p[min(k, D - 1)];
     return v;
 }
-template <class T> __device__ __forceinline__ void store_channels(T *p, int D, typename Pack<T, 4>::type v)
+template <class T, bool NARROW> __device__ __forceinline__ void store_channels(T *p, int D, typename Pack<T, 4>::type v)
 {
-    if (D >= GV) { store_pack<T, 4>(p, v); return; }
+    if constexpr (!NARROW) { store_pack<T, 4>(p, v); return; }
 #pragma unroll
     for (int k = 0; k < GV; ++k) if (k < D) p[k] = v[k];
 }
 
-template <class T> __device__ __forceinline__ void load_steps(typename Pack<T, 4>::type (&v)[GE], const void *base, const ssm_strides &st, const Place &p, int t0, int L, int D)
+// (steps past the end repeat the last one)
+template <class T, bool NARROW> __device__ __forceinline__ void load_steps(typename Pack<T, 4>::type (&v)[GE], const void *base, const ssm_strides &st, const Place &p, int t0, int L, int D)
 {
-    const T *q = static_cast<const T *>(base) + (int64_t)p.seq * st.seq + p.ch;
-    if (D >= GV) {
+    const T *q = static_cast<const T *>(base) + (int64_t)p.seq * st.seq + p.ch + (int64_t)min(t0, L - 1) * st.step;
 #pragma unroll
-        for (int e = 0; e < GE; ++e) v[e] = load_pack<T, 4>(q + (int64_t)min(t0 + e, L - 1) * st.step);
-    } else {
+    for (int e = 0; e < GE; ++e) {
+        v[e] = load_channels<T, NARROW>(q, D);
+        q += t0 + e + 1 < L ? st.step : 0;
+    }
+}
+
+// (values of 16 bits that are needed again stay packed meanwhile)
+template <class T> __device__ __forceinline__ void stay_packed(typename Pack<T, 4>::type (&v)[GE])
+{
+    typedef unsigned words __attribute__((ext_vector_type(2)));
+    if constexpr (sizeof(T) == 2) {
 #pragma unroll
-        for (int e = 0; e < GE; ++e) v[e] = load_channels<T>(q + (int64_t)min(t0 + e, L - 1) * st.step, D);
+        for (int e = 0; e < GE; ++e) {
+            words w = __builtin_bit_cast(words, v[e]);
+            asm volatile("" : "+v"(w));
+            v[e] = __builtin_bit_cast(typename Pack<T, 4>::type, w);
+        }
     }
 }
 
@@ -163,25 +257,29 @@ __device__ __forceinline__ unsigned reset_mask(const GatedArgs &a, const Place &
     if (a.is_first) {
         const uint8_t *q = a.is_first + (int64_t)p.seq * a.L;
 #pragma unroll
-        for (int e = 0; e < GE; ++e) m |= (unsigned)(t0 + e < a.L && q[min(t0 + e, a.L - 1)] != 0) << e;
+        for (int e = 0; e < GE; ++e) m |= (unsigned)(q[min(t0 + e, a.L - 1)] != 0) << e;
+        const int left = a.L - t0;
+        if (left < GE) m &= (1u << max(left, 0)) - 1u;
     }
     return m;
 }
 
-template <class T, bool LINEAR>
+template <class T, bool LINEAR, bool NARROW, bool LOOK>
 __global__ void __launch_bounds__(GATED_MAX_THREADS) gated_fwd_kernel(GatedArgs a)
 {
     __shared__ MapLds lds;
     __shared__ f32x4 s_end[16];              // state at the end of the chunk before
-    const Place p(a);
-    const int cx = 1 << a.lgcx, steps = GE << a.lgtr;
+    int chain = blockIdx.x, first = 0;
+    if constexpr (LOOK) first = take_ticket(a, chain);
+    const Place p(a, chain);
+    const int cx = 1 << a.lgcx, steps = GE * a.rows;
     f32x4 in = {0.f, 0.f, 0.f, 0.f};         // state that flows into the chunk
-    if (a.h0) in = load_channels<float>(a.h0 + (int64_t)p.seq * a.D + p.ch, a.D);
-    for (int tb = 0; tb < a.nTB; ++tb) {
+    if (a.h0) in = load_channels<float, NARROW>(a.h0 + (int64_t)p.seq * a.D + p.ch, a.D);
+    for (int tb = first; tb < (LOOK ? first + 1 : a.nTB); ++tb) {
         const int t0 = tb * steps + p.row * GE;
         typename Pack<T, 4>::type z[GE], u[GE];
-        load_steps<T>(z, a.gate, a.gs, p, t0, a.L, a.D);
-        load_steps<T>(u, a.u, a.us, p, t0, a.L, a.D);
+        load_steps<T, NARROW>(z, a.gate, a.gs, p, t0, a.L, a.D);
+        load_steps<T, NARROW>(u, a.u, a.us, p, t0, a.L, a.D);
         const unsigned cut = reset_mask(a, p, t0);
         f32x4 f[GE], b[GE];
         Map m = identity();
@@ -202,50 +300,54 @@ __global__ void __launch_bounds__(GATED_MAX_THREADS) gated_fwd_kernel(GatedArgs 
             if (p.lane >= 64 - cx) put(lds, p.wave, p.vec, m);
             __syncthreads();
             Map w = identity();
-            for (int k = p.wave0; k < p.wave; ++k) w = after(get(lds, k, p.vec), w);
+            for (int k = 0; k < p.wave; ++k) w = after(get(lds, k, p.vec), w);
+            if constexpr (LOOK) m = after(m, w);
             before = after(before, w);
         }
+        if constexpr (LOOK) in = look_back<true>(a, p, lds, s_end, tb, chain, m, p.row == a.rows - 1, in);
         f32x4 h = apply(before, in);
         if (a.carry && p.stored && t0 > 0 && t0 < a.L && t0 % SSM_GATED_CARRY_STEPS == 0)
-            store_channels<float>(a.carry + ((int64_t)p.seq * a.carry_rows + t0 / SSM_GATED_CARRY_STEPS - 1) * a.D + p.ch, a.D, h);
+            store_channels<float, NARROW>(a.carry + ((int64_t)p.seq * a.carry_rows + t0 / SSM_GATED_CARRY_STEPS - 1) * a.D + p.ch, a.D, h);
         T *out = static_cast<T *>(a.h) + (int64_t)p.seq * a.hs.seq + p.ch;
 #pragma unroll
         for (int e = 0; e < GE; ++e) {
             h = pick4((cut >> e) & 1u, b[e], fma4(f[e], h, b[e]));
             const int t = t0 + e;
             if (p.stored && t < a.L) {
-                store_channels<T>(out + (int64_t)t * a.hs.step, a.D, rounded4<T>(h));
-                if (t == a.L - 1 && a.h_last) store_channels<float>(a.h_last + (int64_t)p.seq * a.D + p.ch, a.D, h);
+                store_channels<T, NARROW>(out + (int64_t)t * a.hs.step, a.D, rounded4<T>(h));
+                if (t == a.L - 1 && a.h_last) store_channels<float, NARROW>(a.h_last + (int64_t)p.seq * a.D + p.ch, a.D, h);
             }
         }
-        if (tb + 1 < a.nTB) {
-            if (p.row == (1 << a.lgtr) - 1) s_end[p.vec] = h;
+        if (!LOOK && tb + 1 < a.nTB) {
+            if (p.row == a.rows - 1) s_end[p.vec] = h;
             __syncthreads();
             in = s_end[p.vec];
         }
     }
 }
 
-template <class T, bool LINEAR>
+template <class T, bool LINEAR, bool NARROW, bool LOOK>
 __global__ void __launch_bounds__(GATED_MAX_THREADS) gated_bwd_kernel(GatedArgs a)
 {
     __shared__ MapLds lds_up, lds_down;
     __shared__ f32x4 s_end[16];
-    const Place p(a);
-    const int cx = 1 << a.lgcx, steps = GE << a.lgtr;
+    int chain = blockIdx.x, first = a.nTB - 1;
+    if constexpr (LOOK) first = a.nTB - 1 - take_ticket(a, chain);
+    const Place p(a, chain);
+    const int cx = 1 << a.lgcx, steps = GE * a.rows;
     const int64_t state = (int64_t)p.seq * a.D + p.ch;
     f32x4 from_right = {0.f, 0.f, 0.f, 0.f};
-    if (a.dh_last) from_right = load_channels<float>(a.dh_last + state, a.D);
-    for (int tb = a.nTB - 1; tb >= 0; --tb) {
+    if (a.dh_last) from_right = load_channels<float, NARROW>(a.dh_last + state, a.D);
+    for (int tb = first; tb >= (LOOK ? first : 0); --tb) {
         const int t0 = tb * steps + p.row * GE;
         typename Pack<T, 4>::type z[GE], u[GE], d[GE];
-        load_steps<T>(d, a.dh, a.dhs, p, t0, a.L, a.D);
-        load_steps<T>(z, a.gate, a.gs, p, t0, a.L, a.D);
-        load_steps<T>(u, a.u, a.us, p, t0, a.L, a.D);
+        load_steps<T, NARROW>(d, a.dh, a.dhs, p, t0, a.L, a.D);
+        load_steps<T, NARROW>(z, a.gate, a.gs, p, t0, a.L, a.D);
+        load_steps<T, NARROW>(u, a.u, a.us, p, t0, a.L, a.D);
         const unsigned cut = reset_mask(a, p, t0);
         f32x4 in = {0.f, 0.f, 0.f, 0.f};
-        if (tb > 0) in = load_channels<float>(a.carry_in + ((int64_t)p.seq * a.carry_rows + tb * steps / SSM_GATED_CARRY_STEPS - 1) * a.D + p.ch, a.D);
-        else if (a.h0) in = load_channels<float>(a.h0 + state, a.D);
+        if (tb > 0) in = load_channels<float, NARROW>(a.carry_in + ((int64_t)p.seq * a.carry_rows + tb * steps / SSM_GATED_CARRY_STEPS - 1) * a.D + p.ch, a.D);
+        else if (a.h0) in = load_channels<float, NARROW>(a.h0 + state, a.D);
         // steps past the end let what flows backwards through: decay 1, no term of their own
         f32x4 f[GE], i[LINEAR ? 1 : GE];
         Map up = identity();
@@ -270,21 +372,28 @@ __global__ void __launch_bounds__(GATED_MAX_THREADS) gated_bwd_kernel(GatedArgs 
             const f32x4 de = pick4(t0 + e >= a.L, f32x4{0.f, 0.f, 0.f, 0.f}, widened4<T>(d[e]));
             down.S = pick4((cut >> e) & 1u, f32x4{0.f, 0.f, 0.f, 0.f}, f[e] * (de + down.S));
         }
+        stay_packed<T>(u);
+        stay_packed<T>(d);
+        __builtin_amdgcn_sched_barrier(0);
         up = inclusive_in_wave<true>(up, p.lane, cx, p.span);
-        down = inclusive_in_wave<false>(down, p.lane, cx, p.span);
         Map before = exclusive_in_wave<true>(up, p.lane, cx, p.span);
+        __builtin_amdgcn_sched_barrier(0);
+        down = inclusive_in_wave<false>(down, p.lane, cx, p.span);
         Map behind = exclusive_in_wave<false>(down, p.lane, cx, p.span);
+        __builtin_amdgcn_sched_barrier(0);
         if (p.waves > 1) {
             if (p.lane >= 64 - cx) put(lds_up, p.wave, p.vec, up);
             if (p.lane < cx) put(lds_down, p.wave, p.vec, down);
             __syncthreads();
             Map w = identity();
-            for (int k = p.wave0; k < p.wave; ++k) w = after(get(lds_up, k, p.vec), w);
+            for (int k = 0; k < p.wave; ++k) w = after(get(lds_up, k, p.vec), w);
             before = after(before, w);
             w = identity();
-            for (int k = p.wave0 + p.waves - 1; k > p.wave; --k) w = after(get(lds_down, k, p.vec), w);
+            for (int k = p.waves - 1; k > p.wave; --k) w = after(get(lds_down, k, p.vec), w);
+            if constexpr (LOOK) down = after(down, w);
             behind = after(behind, w);
         }
+        if constexpr (LOOK) from_right = look_back<false>(a, p, lds_down, s_end, a.nTB - 1 - tb, chain, down, p.row == 0, from_right);
         // chi, last step first
         f32x4 back = apply(behind, from_right), chi[GE];
 #pragma unroll
@@ -309,12 +418,12 @@ __global__ void __launch_bounds__(GATED_MAX_THREADS) gated_bwd_kernel(GatedArgs 
                 h = fma4(f[e], prev, i[e] * ue);
             }
             if (p.stored && t < a.L) {
-                store_channels<T>(du + (int64_t)t * a.dus.step, a.D, rounded4<T>(gu));
-                store_channels<T>(dgate + (int64_t)t * a.dgs.step, a.D, rounded4<T>(gz));
+                store_channels<T, NARROW>(du + (int64_t)t * a.dus.step, a.D, rounded4<T>(gu));
+                store_channels<T, NARROW>(dgate + (int64_t)t * a.dgs.step, a.D, rounded4<T>(gz));
             }
         }
-        if (t0 == 0 && a.dh0 && p.stored) store_channels<float>(a.dh0 + state, a.D, back);
-        if (tb > 0) {
+        if (t0 == 0 && a.dh0 && p.stored) store_channels<float, NARROW>(a.dh0 + state, a.D, back);
+        if (!LOOK && tb > 0) {
             if (p.row == 0) s_end[p.vec] = back;
             __syncthreads();
             from_right = s_end[p.vec];
@@ -338,24 +447,46 @@ __global__ void __launch_bounds__(256) gated_step_kernel(const T *__restrict__ g
     if (y) y[j] = rounded<T>(r);
 }
 
-// Vectors of channels and threads along time of a workgroup, sequences per workgroup.
-struct GatedPlan { int lgcx, lgtr, threads, nCX, nTB; int64_t blocks; };
+// Vectors of channels and threads along time of a workgroup, sequences per workgroup, chunks of a sequence; look: a workgroup per chunk.
+struct GatedPlan { int lgcx, lgspan, rows, seqs, threads, nCX, nTB; bool look; int64_t blocks; size_t ticket_bytes, desc_bytes; };
 GatedPlan plan_gated(int64_t Bt, int64_t L, int64_t D)
 {
-    GatedPlan pl;
+    GatedPlan pl{};
     const int64_t vecs = (D + GV - 1) / GV, rows = (L + GE - 1) / GE;
+    const auto blocks_at = [&](int lg) { return Bt * ((vecs + (1 << lg) - 1) >> lg); };
     pl.lgcx = 0;
     while (pl.lgcx < 4 && (1 << pl.lgcx) < vecs) ++pl.lgcx;
-    pl.lgtr = 0;
-    while ((1 << (pl.lgcx + pl.lgtr)) < GATED_MAX_THREADS && (1 << pl.lgtr) < rows) ++pl.lgtr;
-    const int chunk = 1 << (pl.lgcx + pl.lgtr);
-    pl.threads = chunk < 256 ? 256 : chunk;
-    const int seqs = pl.threads / chunk;
-    pl.nCX = (int)((vecs + (1 << pl.lgcx) - 1) >> pl.lgcx);
-    pl.nTB = (int)((rows + (1 << pl.lgtr) - 1) >> pl.lgtr);
-    pl.blocks = (int64_t)pl.nCX * ((Bt + seqs - 1) / seqs);
+    const int widest = pl.lgcx;
+    while (pl.lgcx > 2 && rows > (GATED_MAX_THREADS >> pl.lgcx) && blocks_at(pl.lgcx) < 512) --pl.lgcx;
+    if (rows > (GATED_MAX_THREADS >> pl.lgcx)) pl.lgcx = widest;
+    const int cx = 1 << pl.lgcx;
+    if (rows * cx <= 64) {                   // a sequence within a wavefront
+        pl.lgspan = pl.lgcx;
+        while ((1 << pl.lgspan) < rows * cx) ++pl.lgspan;
+        pl.rows = 1 << (pl.lgspan - pl.lgcx);
+        pl.threads = 256;
+        while (pl.threads > 64 && (Bt * vecs * pl.rows) / pl.threads < 512) pl.threads /= 2;
+        pl.seqs = pl.threads >> pl.lgspan;
+        pl.nTB = 1;
+    } else {                                 // a sequence, or a chunk of one, per workgroup: whole wavefronts
+        const int per_wave = 64 >> pl.lgcx, most = GATED_MAX_THREADS >> pl.lgcx;
+        pl.lgspan = 6;
+        pl.rows = (int)(rows <= most ? (rows + per_wave - 1) / per_wave * per_wave : most);
+        pl.threads = pl.rows * cx;
+        pl.seqs = 1;
+        pl.nTB = (int)((rows + pl.rows - 1) / pl.rows);
+    }
+    pl.nCX = (int)((vecs + cx - 1) >> pl.lgcx);
+    const int64_t chains = (int64_t)pl.nCX * ((Bt + pl.seqs - 1) / pl.seqs);
+    pl.look = pl.nTB > 1 && chains < 512 && chains * pl.nTB <= 0x7fffffffLL;
+    pl.blocks = pl.look ? chains * pl.nTB : chains;
+    if (pl.look) {
+        pl.ticket_bytes = (size_t)chains * SCAN_TICKET_STRIDE * sizeof(uint32_t);
+        pl.desc_bytes = (size_t)pl.blocks * GATED_DESC_WORDS * sizeof(unsigned long long);
+    }
     return pl;
 }
+constexpr size_t GATED_HEADER = 256;
 
 bool input_strides_ok(const ssm_strides &s) { return s.seq >= 0 && s.step >= 0; }
 // no two elements in one place: steps within sequences, or sequences within steps
@@ -377,18 +508,35 @@ ssm_status check_shape(int dtype, int64_t Bt, int64_t L, int64_t D)
     return SSM_OK;
 }
 
-ssm_status launch_gated(GatedArgs &a, bool reverse, int dtype, int linear, hipStream_t s)
+ssm_status launch_gated(GatedArgs &a, bool reverse, int dtype, int linear, void *workspace, size_t ws_bytes, hipStream_t s)
 {
     const GatedPlan pl = plan_gated(a.Bt, a.L, a.D);
     if (pl.blocks > 0x7fffffffLL) return SSM_ERR_UNSUPPORTED;
-    a.lgcx = pl.lgcx; a.lgtr = pl.lgtr; a.nCX = pl.nCX; a.nTB = pl.nTB; a.carry_rows = (int)ssm_gated_carry_rows(a.L);
+    a.lgcx = pl.lgcx; a.lgspan = pl.lgspan; a.rows = pl.rows; a.seqs = pl.seqs; a.nCX = pl.nCX; a.nTB = pl.nTB;
+    a.carry_rows = (int)ssm_gated_carry_rows(a.L);
+    if (pl.look) {
+        const size_t scratch = pl.ticket_bytes + pl.desc_bytes;
+        if (!workspace || misaligned(workspace, 256) || ws_bytes < GATED_HEADER + scratch) return SSM_ERR_WORKSPACE;
+        char *ws = static_cast<char *>(workspace);
+        a.err = reinterpret_cast<uint32_t *>(ws);
+        a.ticket = reinterpret_cast<uint32_t *>(ws + GATED_HEADER);
+        a.desc = reinterpret_cast<unsigned long long *>(ws + GATED_HEADER + pl.ticket_bytes);
+        a.spin_limit = scan_spin_limit();
+        a.by_chains = FastDiv::by((unsigned)((int64_t)pl.nCX * a.Bt));
+        if (launch_clear(reinterpret_cast<WsHeader *>(ws), ws + GATED_HEADER, scratch, s) != hipSuccess) return SSM_ERR_HIP;
+    }
     const dim3 grid((unsigned)pl.blocks), block((unsigned)pl.threads);
     with_dtype(dtype, [&](auto t) {
         using T = decltype(t);
-        if (reverse && linear) hipLaunchKernelGGL((gated_bwd_kernel<T, true>), grid, block, 0, s, a);
-        else if (reverse) hipLaunchKernelGGL((gated_bwd_kernel<T, false>), grid, block, 0, s, a);
-        else if (linear) hipLaunchKernelGGL((gated_fwd_kernel<T, true>), grid, block, 0, s, a);
-        else hipLaunchKernelGGL((gated_fwd_kernel<T, false>), grid, block, 0, s, a);
+        const auto go = [&](auto lin, auto nar, auto look) {
+            constexpr bool LIN = decltype(lin)::value, NAR = decltype(nar)::value, LOOK = decltype(look)::value;
+            if (reverse) hipLaunchKernelGGL((gated_bwd_kernel<T, LIN, NAR, LOOK>), grid, block, 0, s, a);
+            else hipLaunchKernelGGL((gated_fwd_kernel<T, LIN, NAR, LOOK>), grid, block, 0, s, a);
+        };
+        const std::true_type yes; const std::false_type no;
+        const auto chunks = [&](auto lin, auto nar) { if (pl.look) go(lin, nar, yes); else go(lin, nar, no); };
+        const auto width = [&](auto lin) { if (a.D < GV) chunks(lin, yes); else chunks(lin, no); };
+        if (linear) width(yes); else width(no);
     });
     return hipGetLastError() == hipSuccess ? SSM_OK : SSM_ERR_HIP;
 }
@@ -402,12 +550,17 @@ extern "C" {
 
 int64_t ssm_gated_carry_rows(int64_t L) { return L > 0 ? (L - 1) / SSM_GATED_CARRY_STEPS : 0; }
 
-size_t ssm_gated_workspace_bytes(int64_t, int64_t, int64_t, int, int) { return 0; }
+size_t ssm_gated_workspace_bytes(int64_t Bt, int64_t L, int64_t D, int dtype, int)
+{
+    if (check_shape(dtype, Bt, L, D) != SSM_OK) return 0;
+    const GatedPlan pl = plan_gated(Bt, L, D);
+    return pl.look ? GATED_HEADER + pl.ticket_bytes + pl.desc_bytes : 0;
+}
 
 ssm_status ssm_gated_scan_fwd(const void *gate, ssm_strides gate_strides, const void *u, ssm_strides u_strides,
                               const uint8_t *is_first, const float *h0, int dtype, int linear,
                               int64_t Bt, int64_t L, int64_t D, void *h, ssm_strides h_strides, float *h_last, float *carry,
-                              void *, size_t, void *stream)
+                              void *workspace, size_t ws_bytes, void *stream)
 {
     if (!gate || !u || !h) return SSM_ERR_INVALID_ARG;
     if (const ssm_status rc = check_shape(dtype, Bt, L, D)) return rc;
@@ -420,7 +573,7 @@ ssm_status ssm_gated_scan_fwd(const void *gate, ssm_strides gate_strides, const 
     a.gate = gate; a.gs = gate_strides; a.u = u; a.us = u_strides; a.is_first = is_first; a.h0 = h0;
     a.h = h; a.hs = h_strides; a.h_last = h_last; a.carry = carry;
     a.Bt = (int)Bt; a.L = (int)L; a.D = (int)D;
-    return launch_gated(a, false, dtype, linear, static_cast<hipStream_t>(stream));
+    return launch_gated(a, false, dtype, linear, workspace, ws_bytes, static_cast<hipStream_t>(stream));
 }
 
 ssm_status ssm_gated_scan_bwd(const void *gate, ssm_strides gate_strides, const void *u, ssm_strides u_strides,
@@ -428,7 +581,7 @@ ssm_status ssm_gated_scan_bwd(const void *gate, ssm_strides gate_strides, const 
                               const void *dh, ssm_strides dh_strides, const float *dh_last, int dtype, int linear,
                               int64_t Bt, int64_t L, int64_t D, void *dgate, ssm_strides dgate_strides,
                               void *du, ssm_strides du_strides, float *dh0,
-                              void *, size_t, void *stream)
+                              void *workspace, size_t ws_bytes, void *stream)
 {
     if (!gate || !u || !dh || !dgate || !du) return SSM_ERR_INVALID_ARG;
     if (const ssm_status rc = check_shape(dtype, Bt, L, D)) return rc;
@@ -448,7 +601,7 @@ ssm_status ssm_gated_scan_bwd(const void *gate, ssm_strides gate_strides, const 
     a.dh = dh; a.dhs = dh_strides; a.dh_last = dh_last;
     a.dgate = dgate; a.dgs = dgate_strides; a.du = du; a.dus = du_strides; a.dh0 = dh0;
     a.Bt = (int)Bt; a.L = (int)L; a.D = (int)D;
-    return launch_gated(a, true, dtype, linear, static_cast<hipStream_t>(stream));
+    return launch_gated(a, true, dtype, linear, workspace, ws_bytes, static_cast<hipStream_t>(stream));
 }
 
 ssm_status ssm_gated_step(const void *gate, int64_t gate_pitch, const void *u, int64_t u_pitch, const float *h_prev,
