@@ -10,6 +10,7 @@ namespace ssm {
 
 typedef __bf16 bf16_t;
 typedef _Float16 f16_t;
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // N neighbouring elements; the pointer is aligned to one of them only (rows of any length, halves of an array)

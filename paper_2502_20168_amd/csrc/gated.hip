@@ -17,10 +17,9 @@ namespace {
 
 inline bool misaligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
 
-constexpr int GE = 4;                        // consecutive steps of a thread
-constexpr int GV = 4;                        // neighbouring channels of a thread
-constexpr int GATED_MAX_THREADS = 512;
-
+constexpr int GE = 8;                        // consecutive steps of a thread
+constexpr int GV = 2;                        // neighbouring channels of a thread
+constexpr int GATED_MAX_THREADS = 512, GATED_MAX_VECS = 32;
 struct GatedArgs {
     const void *gate, *u, *dh;
     ssm_strides gs, us, dhs;
@@ -50,68 +49,62 @@ __device__ __forceinline__ Gate gate_of(float z)
     return {f, e > 1.f ? 1.f - f : e * f};
 }
 
-__device__ __forceinline__ f32x4 fma4(f32x4 a, f32x4 b, f32x4 c)
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) { return f32x2{fmaf(a[0], b[0], c[0]), fmaf(a[1], b[1], c[1])}; }
+__device__ __forceinline__ f32x2 pick2(bool c, f32x2 a, f32x2 b) { return f32x2{c ? a[0] : b[0], c ? a[1] : b[1]}; }
+
+// a map over consecutive steps: v -> A v + S, or the constant S where r.  R: whether a reset can be among the steps at all.
+struct Map { f32x2 A, S; int r; };
+__device__ __forceinline__ Map identity() { return {f32x2{1.f, 1.f}, f32x2{0.f, 0.f}, 0}; }
+template <bool R> __device__ __forceinline__ Map after(const Map &y, const Map &x)      // x first, then y
 {
-    f32x4 r;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) r[k] = fmaf(a[k], b[k], c[k]);
-    return r;
+    const f32x2 s = fma2(y.A, x.S, y.S);
+    return {y.A * x.A, R ? pick2(y.r, y.S, s) : s, R ? y.r | x.r : 0};
 }
-__device__ __forceinline__ f32x4 pick4(bool c, f32x4 a, f32x4 b)
+__device__ __forceinline__ f32x2 apply(const Map &m, f32x2 v) { return pick2(m.r, m.S, fma2(m.A, v, m.S)); }
+template <bool R> __device__ __forceinline__ Map pick(bool c, const Map &a, const Map &b) { return {pick2(c, a.A, b.A), pick2(c, a.S, b.S), R ? (c ? a.r : b.r) : 0}; }
+template <bool UP, bool R> __device__ __forceinline__ Map neighbour(const Map &m, int d)
 {
-    f32x4 r;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) r[k] = c ? a[k] : b[k];
-    return r;
-}
-__device__ __forceinline__ f32x4 up4(f32x4 v, int d)
-{
-    f32x4 r;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) r[k] = __shfl_up(v[k], d);
-    return r;
-}
-__device__ __forceinline__ f32x4 down4(f32x4 v, int d)
-{
-    f32x4 r;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) r[k] = __shfl_down(v[k], d);
-    return r;
+    const auto of = [&](float v) { return UP ? __shfl_up(v, d) : __shfl_down(v, d); };
+    return {f32x2{of(m.A[0]), of(m.A[1])}, f32x2{of(m.S[0]), of(m.S[1])}, R ? (UP ? __shfl_up(m.r, d) : __shfl_down(m.r, d)) : 0};
 }
 
-// a map over consecutive steps: v -> A v + S, or the constant S where r
-struct Map { f32x4 A, S; int r; };
-__device__ __forceinline__ Map identity() { return {f32x4{1.f, 1.f, 1.f, 1.f}, f32x4{0.f, 0.f, 0.f, 0.f}, 0}; }
-__device__ __forceinline__ Map after(const Map &y, const Map &x)      // x first, then y
-{
-    return {y.A * x.A, pick4(y.r, y.S, fma4(y.A, x.S, y.S)), y.r | x.r};
-}
-__device__ __forceinline__ f32x4 apply(const Map &m, f32x4 v) { return pick4(m.r, m.S, fma4(m.A, v, m.S)); }
-__device__ __forceinline__ Map pick(bool c, const Map &a, const Map &b) { return {pick4(c, a.A, b.A), pick4(c, a.S, b.S), c ? a.r : b.r}; }
-
-// Exclusive composition over the threads along time of a chunk: of the earlier ones (UP) or the later ones.  `lds`: a map per wavefront and vector of channels.
-struct MapLds { f32x4 A[GATED_MAX_THREADS / 64][16], S[GATED_MAX_THREADS / 64][16]; int r[GATED_MAX_THREADS / 64][16]; };
-template <bool UP> __device__ __forceinline__ Map inclusive_in_wave(Map m, int lane, int cx, int span)
+// Composition over the threads along time of a chunk: within a wavefront between lanes, over wavefronts in LDS (a map per wavefront and vector of channels; the
+// flag is the same for all channels of a sequence).
+struct MapLds { f32x4 m[GATED_MAX_THREADS / 64][GATED_MAX_VECS]; int r[GATED_MAX_THREADS / 64]; };
+template <bool UP, bool R> __device__ __forceinline__ Map inclusive_in_wave(Map m, int lane, int cx, int span)
 {
     const int l = lane & (span - 1);
-    for (int d = cx; d < span; d <<= 1) {
-        Map o;
-        if constexpr (UP) o = {up4(m.A, d), up4(m.S, d), __shfl_up(m.r, d)};
-        else o = {down4(m.A, d), down4(m.S, d), __shfl_down(m.r, d)};
-        m = pick(UP ? l >= d : l + d < span, after(m, o), m);
-    }
+    for (int d = cx; d < span; d <<= 1) m = pick<R>(UP ? l >= d : l + d < span, after<R>(m, neighbour<UP, R>(m, d)), m);
     return m;
 }
-template <bool UP> __device__ __forceinline__ Map exclusive_in_wave(const Map &incl, int lane, int cx, int span)
+template <bool UP, bool R> __device__ __forceinline__ Map exclusive_in_wave(const Map &incl, int lane, int cx, int span)
 {
     const int l = lane & (span - 1);
-    Map o;
-    if constexpr (UP) o = {up4(incl.A, cx), up4(incl.S, cx), __shfl_up(incl.r, cx)};
-    else o = {down4(incl.A, cx), down4(incl.S, cx), __shfl_down(incl.r, cx)};
-    return pick(UP ? l >= cx : l + cx < span, o, identity());
+    return pick<R>(UP ? l >= cx : l + cx < span, neighbour<UP, R>(incl, cx), identity());
 }
-__device__ __forceinline__ void put(MapLds &s, int w, int c, const Map &m) { s.A[w][c] = m.A; s.S[w][c] = m.S; s.r[w][c] = m.r; }
-__device__ __forceinline__ Map get(const MapLds &s, int w, int c) { return {s.A[w][c], s.S[w][c], s.r[w][c]}; }
+__device__ __forceinline__ void put(MapLds &s, int w, int c, const Map &m)
+{
+    s.m[w][c] = f32x4{m.A[0], m.A[1], m.S[0], m.S[1]};
+    if (c == 0) s.r[w] = m.r;
+}
+__device__ __forceinline__ Map get(const MapLds &s, int w, int c)
+{
+    const f32x4 q = s.m[w][c];
+    return {f32x2{q[0], q[1]}, f32x2{q[2], q[3]}, s.r[w]};
+}
+// the maps of wavefronts 0 .. n-1 (UP) or waves-1 .. waves-n, the first one first.  (Four are read at a time: one by one, every step would wait for LDS.)
+template <bool UP> __device__ __forceinline__ Map fold(const MapLds &s, int c, int n, int waves)
+{
+    Map w = identity();
+    for (int k0 = 0; k0 < n; k0 += 4) {
+        Map q[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) { const int i = min(k0 + k, n - 1); q[k] = get(s, UP ? i : waves - 1 - i, c); }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) if (k0 + k < n) w = after<true>(q[k], w);
+    }
+    return w;
+}
 
 // What a thread owns: GE steps of GV channels of one sequence.  Threads past the end of an axis take the last valid place and store nothing.
 // The last vector of a row is moved back so that it ends with the row: its channels are computed twice, with the same operations, and the same values stored twice.
@@ -123,7 +116,7 @@ struct Place {
         const int tid = threadIdx.x, cx = 1 << a.lgcx;
         const bool several = a.seqs > 1;
         lane = tid & 63;
-        wave = tid >> 6;
+        wave = __builtin_amdgcn_readfirstlane(tid >> 6);
         span = 1 << a.lgspan;
         vec = tid & (cx - 1);
         row = (several ? tid & (span - 1) : tid) >> a.lgcx;
@@ -140,39 +133,35 @@ struct Place {
 // each of its rows fetches the map of one earlier chunk of its group of `rows` chunks, all at once, and one row the state behind the last chunk of
 // the group before.  The order of the compositions is fixed, whatever the timing: results are repeatable.  Chunks are numbered by a ticket per chain (the chunks of one
 // sequence and channel block), so that a workgroup waits for such as have started; a wait that gives up hands on NaN and says so in the workspace.
-__device__ __forceinline__ bool wait_words(const unsigned long long *w, unsigned limit, f32x4 &v, unsigned &tag)
+__device__ __forceinline__ bool wait_words(const unsigned long long *w, unsigned limit, f32x2 &v, unsigned &tag)
 {
     for (unsigned spins = 0;; ++spins) {
-        unsigned long long q[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) q[k] = poll_word(w + k);
-        bool all = true;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) { all = all && word_tag(q[k]) != 0; v[k] = word_value(q[k]); }
-        tag = word_tag(q[0]);
-        if (all) return true;
+        const unsigned long long a = poll_word(w), b = poll_word(w + 1);
+        v = f32x2{word_value(a), word_value(b)};
+        tag = word_tag(a);
+        if (tag != 0 && word_tag(b) != 0) return true;
         if (spins >= limit) return false;
         __builtin_amdgcn_s_sleep(2);
     }
 }
-__device__ __forceinline__ void publish4(unsigned long long *w, f32x4 v, unsigned tag)
+__device__ __forceinline__ void publish2(unsigned long long *w, f32x2 v, unsigned tag)
 {
-#pragma unroll
-    for (int k = 0; k < 4; ++k) publish_word(w + k, v[k], tag);
+    publish_word(w, v[0], tag);
+    publish_word(w + 1, v[1], tag);
 }
 // UP: rows in the order of time.  `chunk`: number along the direction of the scan; `total`: the chunk's map, valid where `ends`; v0: what flows into the first chunk.
-template <bool UP> __device__ __forceinline__ f32x4 look_back(const GatedArgs &a, const Place &p, MapLds &lds, f32x4 *s_base, int chunk, int chain, const Map &total, bool ends, f32x4 v0)
+template <bool UP> __device__ __forceinline__ f32x2 look_back(const GatedArgs &a, const Place &p, MapLds &lds, f32x2 *s_base, int chunk, int chain, const Map &total, bool ends, f32x2 v0)
 {
     const int cx = 1 << a.lgcx, chains = a.nCX * a.Bt, group = chunk / a.rows * a.rows, row = UP ? p.row : a.rows - 1 - p.row;
     unsigned long long *mine = a.desc + ((int64_t)chunk * chains + chain) * GATED_DESC_WORDS + p.vec * GV;
     const int64_t back = (int64_t)chains * GATED_DESC_WORDS;
     if (ends && chunk + 1 < a.nTB) {
-        publish4(mine, total.A, 1);
-        publish4(mine + 64, total.S, total.r ? 2 : 1);
+        publish2(mine, total.A, 1);
+        publish2(mine + 64, total.S, total.r ? 2 : 1);
     }
-    f32x4 v = v0;
+    f32x2 v = v0;
     if (chunk > 0) {                         // (uniform)
-        const f32x4 nan = {__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
+        const f32x2 nan = {__builtin_nanf(""), __builtin_nanf("")};
         Map m = identity();
         if (group + row < chunk) {
             const unsigned long long *w = mine - (chunk - group - row) * back;
@@ -183,19 +172,17 @@ template <bool UP> __device__ __forceinline__ f32x4 look_back(const GatedArgs &a
         }
         if (group > 0 && row == 0) {
             unsigned tag;
-            f32x4 base;
+            f32x2 base;
             if (!wait_words(mine - (chunk - group + 1) * back + 128, a.spin_limit, base, tag)) { atomicOr(a.err, 1u); base = nan; }
             s_base[p.vec] = base;
         }
-        m = inclusive_in_wave<UP>(m, p.lane, cx, p.span);
+        m = inclusive_in_wave<UP, true>(m, p.lane, cx, p.span);
         __syncthreads();                     // (the maps of the chunk itself have been read)
         if (UP ? p.lane >= 64 - cx : p.lane < cx) put(lds, p.wave, p.vec, m);
         __syncthreads();
-        Map w = identity();
-        for (int k = 0; k < p.waves; ++k) w = after(get(lds, UP ? k : p.waves - 1 - k, p.vec), w);
-        v = apply(w, group > 0 ? s_base[p.vec] : v0);
+        v = apply(fold<UP>(lds, p.vec, p.waves, p.waves), group > 0 ? s_base[p.vec] : v0);
     }
-    if (ends && chunk + 1 < a.nTB && (chunk + 1) % a.rows == 0) publish4(mine + 128, apply(total, v), 3);
+    if (ends && chunk + 1 < a.nTB && (chunk + 1) % a.rows == 0) publish2(mine + 128, apply(total, v), 3);
     return v;
 }
 // the chunk and the chain of this workgroup
@@ -209,114 +196,150 @@ __device__ __forceinline__ int take_ticket(const GatedArgs &a, int &chain)
     return __builtin_amdgcn_readfirstlane(s_chunk);
 }
 
-// NARROW: rows of fewer than GV channels, whose one vector repeats the last of them.
-template <class T, bool NARROW> __device__ __forceinline__ typename Pack<T, 4>::type load_channels(const T *p, int D)
+// NARROW: a single channel, held twice.
+template <class T, bool NARROW> __device__ __forceinline__ typename Pack<T, 2>::type load_channels(const T *p)
 {
-    if constexpr (!NARROW) return load_pack<T, 4>(p);
-    typename Pack<T, 4>::type v;
-#pragma unroll
-    for (int k = 0; k < GV; ++k) v[k] = p[min(k, D - 1)];
-    return v;
+    if constexpr (!NARROW) return load_pack<T, 2>(p);
+    else return typename Pack<T, 2>::type{p[0], p[0]};
 }
-template <class T, bool NARROW> __device__ __forceinline__ void store_channels(T *p, int D, typename Pack<T, 4>::type v)
+template <class T, bool NARROW> __device__ __forceinline__ void store_channels(T *p, f32x2 v)
 {
-    if constexpr (!NARROW) { store_pack<T, 4>(p, v); return; }
-#pragma unroll
-    for (int k = 0; k < GV; ++k) if (k < D) p[k] = v[k];
+    const typename Pack<T, 2>::type q = __builtin_convertvector(v, typename Pack<T, 2>::type);
+    if constexpr (!NARROW) store_pack<T, 2>(p, q);
+    else p[0] = q[0];
 }
-
+template <class T> __device__ __forceinline__ const T *first_step(const void *base, const ssm_strides &st, const Place &p, int t)
+{
+    return static_cast<const T *>(base) + (int64_t)p.seq * st.seq + (int64_t)t * st.step + p.ch;
+}
 // (steps past the end repeat the last one)
-template <class T, bool NARROW> __device__ __forceinline__ void load_steps(typename Pack<T, 4>::type (&v)[GE], const void *base, const ssm_strides &st, const Place &p, int t0, int L, int D)
+template <class T, bool NARROW> __device__ __forceinline__ void load_steps(typename Pack<T, 2>::type (&v)[GE], const void *base, const ssm_strides &st, const Place &p, int t0, int L, bool full)
 {
-    const T *q = static_cast<const T *>(base) + (int64_t)p.seq * st.seq + p.ch + (int64_t)min(t0, L - 1) * st.step;
+    const T *q = first_step<T>(base, st, p, min(t0, L - 1));
+    if (full) {                              // (uniform)
 #pragma unroll
-    for (int e = 0; e < GE; ++e) {
-        v[e] = load_channels<T, NARROW>(q, D);
-        q += t0 + e + 1 < L ? st.step : 0;
-    }
-}
-
-// (values of 16 bits that are needed again stay packed meanwhile)
-template <class T> __device__ __forceinline__ void stay_packed(typename Pack<T, 4>::type (&v)[GE])
-{
-    typedef unsigned words __attribute__((ext_vector_type(2)));
-    if constexpr (sizeof(T) == 2) {
+        for (int e = 0; e < GE; ++e) v[e] = load_channels<T, NARROW>(q + e * st.step);
+    } else {
 #pragma unroll
         for (int e = 0; e < GE; ++e) {
-            words w = __builtin_bit_cast(words, v[e]);
-            asm volatile("" : "+v"(w));
-            v[e] = __builtin_bit_cast(typename Pack<T, 4>::type, w);
+            v[e] = load_channels<T, NARROW>(q);
+            q += t0 + e + 1 < L ? st.step : 0;
         }
+    }
+}
+template <class T, bool NARROW> __device__ __forceinline__ void store_steps(const f32x2 (&v)[GE], void *base, const ssm_strides &st, const Place &p, int t0, int L, bool full)
+{
+    T *q = const_cast<T *>(first_step<T>(base, st, p, t0));
+    if (!p.stored) return;
+    if (full) {
+#pragma unroll
+        for (int e = 0; e < GE; ++e) store_channels<T, NARROW>(q + e * st.step, v[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < GE; ++e) if (t0 + e < L) store_channels<T, NARROW>(q + e * st.step, v[e]);
     }
 }
 
 // flags of a thread's steps, bit e = the state that flows into step t0 + e is dropped
-__device__ __forceinline__ unsigned reset_mask(const GatedArgs &a, const Place &p, int t0)
+__device__ __forceinline__ unsigned reset_mask(const GatedArgs &a, const Place &p, int t0, bool full)
 {
+    if (!a.is_first) return 0;
+    const uint8_t *q = a.is_first + (int64_t)p.seq * a.L;
     unsigned m = 0;
-    if (a.is_first) {
-        const uint8_t *q = a.is_first + (int64_t)p.seq * a.L;
+    if (full) {
+        typedef unsigned long long loose __attribute__((aligned(1)));
+        const unsigned long long w = *reinterpret_cast<const loose *>(q + t0);
+        if (w == 0) return 0;
 #pragma unroll
-        for (int e = 0; e < GE; ++e) m |= (unsigned)(q[min(t0 + e, a.L - 1)] != 0) << e;
-        const int left = a.L - t0;
-        if (left < GE) m &= (1u << max(left, 0)) - 1u;
+        for (int e = 0; e < GE; ++e) m |= (unsigned)(((w >> (8 * e)) & 255u) != 0) << e;
+        return m;
     }
-    return m;
+#pragma unroll
+    for (int e = 0; e < GE; ++e) m |= (unsigned)(q[min(t0 + e, a.L - 1)] != 0) << e;
+    const int left = a.L - t0;
+    return left < GE ? m & ((1u << max(left, 0)) - 1u) : m;
+}
+
+template <class T, bool LINEAR> __device__ __forceinline__ void gates(const typename Pack<T, 2>::type (&z)[GE], f32x2 (&f)[GE], f32x2 (&i)[GE])
+{
+#pragma unroll
+    for (int e = 0; e < GE; ++e) {
+        const f32x2 ze = __builtin_convertvector(z[e], f32x2);
+        if constexpr (LINEAR) {
+            f[e] = ze;
+        } else {
+            const Gate a = gate_of(ze[0]), b = gate_of(ze[1]);
+            f[e] = f32x2{a.f, b.f};
+            i[e] = f32x2{a.i, b.i};
+        }
+    }
+}
+template <class F> __device__ __forceinline__ void if_resets(bool plain, F f)
+{
+    if (plain) f(std::false_type{}); else f(std::true_type{});
 }
 
 template <class T, bool LINEAR, bool NARROW, bool LOOK>
 __global__ void __launch_bounds__(GATED_MAX_THREADS) gated_fwd_kernel(GatedArgs a)
 {
     __shared__ MapLds lds;
-    __shared__ f32x4 s_end[16];              // state at the end of the chunk before
+    __shared__ f32x2 s_end[GATED_MAX_VECS];  // state at the end of the chunk before
     int chain = blockIdx.x, first = 0;
     if constexpr (LOOK) first = take_ticket(a, chain);
     const Place p(a, chain);
     const int cx = 1 << a.lgcx, steps = GE * a.rows;
-    f32x4 in = {0.f, 0.f, 0.f, 0.f};         // state that flows into the chunk
-    if (a.h0) in = load_channels<float, NARROW>(a.h0 + (int64_t)p.seq * a.D + p.ch, a.D);
+    const int64_t state = (int64_t)p.seq * a.D + p.ch;
+    f32x2 in = {0.f, 0.f};                   // state that flows into the chunk
+    if (a.h0) in = load_channels<float, NARROW>(a.h0 + state);
     for (int tb = first; tb < (LOOK ? first + 1 : a.nTB); ++tb) {
         const int t0 = tb * steps + p.row * GE;
-        typename Pack<T, 4>::type z[GE], u[GE];
-        load_steps<T, NARROW>(z, a.gate, a.gs, p, t0, a.L, a.D);
-        load_steps<T, NARROW>(u, a.u, a.us, p, t0, a.L, a.D);
-        const unsigned cut = reset_mask(a, p, t0);
-        f32x4 f[GE], b[GE];
-        Map m = identity();
+        const bool full = (tb + 1) * steps <= a.L;
+        typename Pack<T, 2>::type z[GE], u[GE];
+        load_steps<T, NARROW>(z, a.gate, a.gs, p, t0, a.L, full);
+        load_steps<T, NARROW>(u, a.u, a.us, p, t0, a.L, full);
+        const unsigned cut = reset_mask(a, p, t0, full);
+        const bool plain = __builtin_amdgcn_ballot_w64(cut != 0) == 0;
+        f32x2 f[GE], b[GE];
+        gates<T, LINEAR>(z, f, b);
 #pragma unroll
         for (int e = 0; e < GE; ++e) {
-            const f32x4 ze = widened4<T>(z[e]), ue = widened4<T>(u[e]);
-            if constexpr (LINEAR) {
-                f[e] = ze; b[e] = ue;
-            } else {
-#pragma unroll
-                for (int k = 0; k < GV; ++k) { const Gate g = gate_of(ze[k]); f[e][k] = g.f; b[e][k] = g.i * ue[k]; }
-            }
-            m = after(Map{f[e], b[e], (int)((cut >> e) & 1u)}, m);
+            const f32x2 ue = __builtin_convertvector(u[e], f32x2);
+            b[e] = LINEAR ? ue : b[e] * ue;
         }
-        m = inclusive_in_wave<true>(m, p.lane, cx, p.span);
-        Map before = exclusive_in_wave<true>(m, p.lane, cx, p.span);
+        Map m, before;
+        if_resets(plain, [&](auto r) {
+            constexpr bool R = decltype(r)::value;
+            m = identity();
+#pragma unroll
+            for (int e = 0; e < GE; ++e) m = after<R>(Map{f[e], b[e], (int)((cut >> e) & 1u)}, m);
+            m = inclusive_in_wave<true, R>(m, p.lane, cx, p.span);
+            before = exclusive_in_wave<true, R>(m, p.lane, cx, p.span);
+        });
         if (p.waves > 1) {                   // (uniform)
             if (p.lane >= 64 - cx) put(lds, p.wave, p.vec, m);
             __syncthreads();
-            Map w = identity();
-            for (int k = 0; k < p.wave; ++k) w = after(get(lds, k, p.vec), w);
-            if constexpr (LOOK) m = after(m, w);
-            before = after(before, w);
+            const Map w = fold<true>(lds, p.vec, p.wave, p.waves);
+            if constexpr (LOOK) m = after<true>(m, w);
+            before = after<true>(before, w);
         }
         if constexpr (LOOK) in = look_back<true>(a, p, lds, s_end, tb, chain, m, p.row == a.rows - 1, in);
-        f32x4 h = apply(before, in);
+        f32x2 h = apply(before, in);
         if (a.carry && p.stored && t0 > 0 && t0 < a.L && t0 % SSM_GATED_CARRY_STEPS == 0)
-            store_channels<float, NARROW>(a.carry + ((int64_t)p.seq * a.carry_rows + t0 / SSM_GATED_CARRY_STEPS - 1) * a.D + p.ch, a.D, h);
-        T *out = static_cast<T *>(a.h) + (int64_t)p.seq * a.hs.seq + p.ch;
+            store_channels<float, NARROW>(a.carry + ((int64_t)p.seq * a.carry_rows + t0 / SSM_GATED_CARRY_STEPS - 1) * a.D + p.ch, h);
+        if_resets(plain, [&](auto r) {
+            constexpr bool R = decltype(r)::value;
 #pragma unroll
-        for (int e = 0; e < GE; ++e) {
-            h = pick4((cut >> e) & 1u, b[e], fma4(f[e], h, b[e]));
-            const int t = t0 + e;
-            if (p.stored && t < a.L) {
-                store_channels<T, NARROW>(out + (int64_t)t * a.hs.step, a.D, rounded4<T>(h));
-                if (t == a.L - 1 && a.h_last) store_channels<float, NARROW>(a.h_last + (int64_t)p.seq * a.D + p.ch, a.D, h);
+            for (int e = 0; e < GE; ++e) {
+                h = R ? pick2((cut >> e) & 1u, b[e], fma2(f[e], h, b[e])) : fma2(f[e], h, b[e]);
+                b[e] = h;
             }
+        });
+        store_steps<T, NARROW>(b, a.h, a.hs, p, t0, a.L, full);
+        if (a.h_last && p.stored && t0 < a.L && a.L - t0 <= GE) {
+            f32x2 last = b[0];
+#pragma unroll
+            for (int e = 1; e < GE; ++e) last = pick2(t0 + e < a.L, b[e], last);
+            store_channels<float, NARROW>(a.h_last + state, last);
         }
         if (!LOOK && tb + 1 < a.nTB) {
             if (p.row == a.rows - 1) s_end[p.vec] = h;
@@ -327,102 +350,106 @@ __global__ void __launch_bounds__(GATED_MAX_THREADS) gated_fwd_kernel(GatedArgs 
 }
 
 template <class T, bool LINEAR, bool NARROW, bool LOOK>
-__global__ void __launch_bounds__(GATED_MAX_THREADS) gated_bwd_kernel(GatedArgs a)
+__global__ void __launch_bounds__(GATED_MAX_THREADS, 4) gated_bwd_kernel(GatedArgs a)
 {
     __shared__ MapLds lds_up, lds_down;
-    __shared__ f32x4 s_end[16];
+    __shared__ f32x2 s_end[GATED_MAX_VECS];
     int chain = blockIdx.x, first = a.nTB - 1;
     if constexpr (LOOK) first = a.nTB - 1 - take_ticket(a, chain);
-    const Place p(a, chain);
+    Place p(a, chain);
     const int cx = 1 << a.lgcx, steps = GE * a.rows;
-    const int64_t state = (int64_t)p.seq * a.D + p.ch;
-    f32x4 from_right = {0.f, 0.f, 0.f, 0.f};
-    if (a.dh_last) from_right = load_channels<float, NARROW>(a.dh_last + state, a.D);
+    const f32x2 zero = {0.f, 0.f};
+    f32x2 from_right = zero;
+    if (a.dh_last) from_right = load_channels<float, NARROW>(a.dh_last + (int64_t)p.seq * a.D + p.ch);
     for (int tb = first; tb >= (LOOK ? first : 0); --tb) {
+        asm volatile("" : "+v"(p.seq), "+v"(p.ch));          // (addresses are formed where they are used, not kept from one chunk to the next)
+        const int64_t state = (int64_t)p.seq * a.D + p.ch;
         const int t0 = tb * steps + p.row * GE;
-        typename Pack<T, 4>::type z[GE], u[GE], d[GE];
-        load_steps<T, NARROW>(d, a.dh, a.dhs, p, t0, a.L, a.D);
-        load_steps<T, NARROW>(z, a.gate, a.gs, p, t0, a.L, a.D);
-        load_steps<T, NARROW>(u, a.u, a.us, p, t0, a.L, a.D);
-        const unsigned cut = reset_mask(a, p, t0);
-        f32x4 in = {0.f, 0.f, 0.f, 0.f};
-        if (tb > 0) in = load_channels<float, NARROW>(a.carry_in + ((int64_t)p.seq * a.carry_rows + tb * steps / SSM_GATED_CARRY_STEPS - 1) * a.D + p.ch, a.D);
-        else if (a.h0) in = load_channels<float, NARROW>(a.h0 + state, a.D);
-        // steps past the end let what flows backwards through: decay 1, no term of their own
-        f32x4 f[GE], i[LINEAR ? 1 : GE];
-        Map up = identity();
+        const bool full = (tb + 1) * steps <= a.L;
+        f32x2 f[GE], i[GE], u[GE], d[GE];
+        {
+            typename Pack<T, 2>::type rz[GE], ru[GE], rd[GE];
+            load_steps<T, NARROW>(rz, a.gate, a.gs, p, t0, a.L, full);
+            load_steps<T, NARROW>(ru, a.u, a.us, p, t0, a.L, full);
+            load_steps<T, NARROW>(rd, a.dh, a.dhs, p, t0, a.L, full);
+            gates<T, LINEAR>(rz, f, i);
+#pragma unroll
+            for (int e = 0; e < GE; ++e) { u[e] = __builtin_convertvector(ru[e], f32x2); d[e] = __builtin_convertvector(rd[e], f32x2); }
+        }
+        const unsigned cut = reset_mask(a, p, t0, full);
+        const bool plain = __builtin_amdgcn_ballot_w64(cut != 0) == 0;
+        f32x2 in = zero;
+        if (tb > 0) in = load_channels<float, NARROW>(a.carry_in + ((int64_t)p.seq * a.carry_rows + tb * steps / SSM_GATED_CARRY_STEPS - 1) * a.D + p.ch);
+        else if (a.h0) in = load_channels<float, NARROW>(a.h0 + state);
+        if (!full) {                         // steps past the end let what flows backwards through: decay 1, no term of their own
+#pragma unroll
+            for (int e = 0; e < GE; ++e) {
+                const bool past = t0 + e >= a.L;
+                f[e] = pick2(past, f32x2{1.f, 1.f}, f[e]);
+                d[e] = pick2(past, zero, d[e]);
+            }
+        }
+        // (pinned: the compiler otherwise keeps products of these beside them, 20 registers more, one wavefront of a SIMD fewer)
 #pragma unroll
         for (int e = 0; e < GE; ++e) {
-            const f32x4 ze = widened4<T>(z[e]), ue = widened4<T>(u[e]);
-            const bool past = t0 + e >= a.L;
-            f32x4 b;
-            if constexpr (LINEAR) {
-                f[e] = ze; b = ue;
-            } else {
+            asm volatile("" : "+v"(f[e]), "+v"(u[e]), "+v"(d[e]));
+            if constexpr (!LINEAR) asm volatile("" : "+v"(i[e]));
+        }
+        Map up, down, before, behind;
+        if_resets(plain, [&](auto r) {
+            constexpr bool R = decltype(r)::value;
+            up = identity();
 #pragma unroll
-                for (int k = 0; k < GV; ++k) { const Gate g = gate_of(ze[k]); f[e][k] = g.f; i[e][k] = g.i; }
-                b = i[e] * ue;
+            for (int e = 0; e < GE; ++e) up = after<R>(Map{f[e], LINEAR ? u[e] : i[e] * u[e], (int)((cut >> e) & 1u)}, up);
+            down = {up.A, zero, up.r};
+#pragma unroll
+            for (int e = GE - 1; e >= 0; --e) {
+                const f32x2 back = f[e] * (d[e] + down.S);
+                down.S = R ? pick2((cut >> e) & 1u, zero, back) : back;
             }
-            f[e] = pick4(past, f32x4{1.f, 1.f, 1.f, 1.f}, f[e]);
-            up = after(Map{f[e], b, (int)((cut >> e) & 1u)}, up);
-        }
-        Map down = {up.A, f32x4{0.f, 0.f, 0.f, 0.f}, up.r};
-#pragma unroll
-        for (int e = GE - 1; e >= 0; --e) {
-            const f32x4 de = pick4(t0 + e >= a.L, f32x4{0.f, 0.f, 0.f, 0.f}, widened4<T>(d[e]));
-            down.S = pick4((cut >> e) & 1u, f32x4{0.f, 0.f, 0.f, 0.f}, f[e] * (de + down.S));
-        }
-        stay_packed<T>(u);
-        stay_packed<T>(d);
-        __builtin_amdgcn_sched_barrier(0);
-        up = inclusive_in_wave<true>(up, p.lane, cx, p.span);
-        Map before = exclusive_in_wave<true>(up, p.lane, cx, p.span);
-        __builtin_amdgcn_sched_barrier(0);
-        down = inclusive_in_wave<false>(down, p.lane, cx, p.span);
-        Map behind = exclusive_in_wave<false>(down, p.lane, cx, p.span);
-        __builtin_amdgcn_sched_barrier(0);
+            up = inclusive_in_wave<true, R>(up, p.lane, cx, p.span);
+            before = exclusive_in_wave<true, R>(up, p.lane, cx, p.span);
+            down = inclusive_in_wave<false, R>(down, p.lane, cx, p.span);
+            behind = exclusive_in_wave<false, R>(down, p.lane, cx, p.span);
+        });
         if (p.waves > 1) {
             if (p.lane >= 64 - cx) put(lds_up, p.wave, p.vec, up);
             if (p.lane < cx) put(lds_down, p.wave, p.vec, down);
             __syncthreads();
-            Map w = identity();
-            for (int k = 0; k < p.wave; ++k) w = after(get(lds_up, k, p.vec), w);
-            before = after(before, w);
-            w = identity();
-            for (int k = p.waves - 1; k > p.wave; --k) w = after(get(lds_down, k, p.vec), w);
-            if constexpr (LOOK) down = after(down, w);
-            behind = after(behind, w);
+            before = after<true>(before, fold<true>(lds_up, p.vec, p.wave, p.waves));
+            const Map w = fold<false>(lds_down, p.vec, p.waves - 1 - p.wave, p.waves);
+            if constexpr (LOOK) down = after<true>(down, w);
+            behind = after<true>(behind, w);
         }
         if constexpr (LOOK) from_right = look_back<false>(a, p, lds_down, s_end, a.nTB - 1 - tb, chain, down, p.row == 0, from_right);
-        // chi, last step first
-        f32x4 back = apply(behind, from_right), chi[GE];
+        f32x2 back = apply(behind, from_right), h = apply(before, in);
+        if_resets(plain, [&](auto r) {
+            constexpr bool R = decltype(r)::value;
+            // chi, last step first (in place of dh)
 #pragma unroll
-        for (int e = GE - 1; e >= 0; --e) {
-            const bool past = t0 + e >= a.L;
-            chi[e] = widened4<T>(d[e]) + back;
-            back = pick4((cut >> e) & 1u, f32x4{0.f, 0.f, 0.f, 0.f}, pick4(past, back, f[e] * chi[e]));
-        }
-        // the states again, first step first, and the gradients
-        f32x4 h = apply(before, in);
-        T *dgate = static_cast<T *>(a.dgate) + (int64_t)p.seq * a.dgs.seq + p.ch, *du = static_cast<T *>(a.du) + (int64_t)p.seq * a.dus.seq + p.ch;
+            for (int e = GE - 1; e >= 0; --e) {
+                d[e] += back;
+                back = R ? pick2((cut >> e) & 1u, zero, f[e] * d[e]) : f[e] * d[e];
+            }
+            // the states again, first step first, and the gradients (du in place of chi, dgate in place of u)
 #pragma unroll
-        for (int e = 0; e < GE; ++e) {
-            const int t = t0 + e;
-            const f32x4 ue = widened4<T>(u[e]), prev = pick4((cut >> e) & 1u, f32x4{0.f, 0.f, 0.f, 0.f}, h);
-            f32x4 gu, gz;
-            if constexpr (LINEAR) {
-                gu = chi[e]; gz = prev * chi[e];
-                h = fma4(f[e], prev, ue);
-            } else {
-                gu = i[e] * chi[e]; gz = f[e] * (prev - ue) * gu;
-                h = fma4(f[e], prev, i[e] * ue);
+            for (int e = 0; e < GE; ++e) {
+                const f32x2 prev = R ? pick2((cut >> e) & 1u, zero, h) : h;
+                if constexpr (LINEAR) {
+                    h = fma2(f[e], prev, u[e]);
+                    u[e] = prev * d[e];
+                } else {
+                    // f prev + (1 - f) u = u + f (prev - u): rounded by u's last place, which is what prev - u has anyway
+                    const f32x2 w = prev - u[e];
+                    h = fma2(f[e], w, u[e]);
+                    d[e] *= i[e];
+                    u[e] = f[e] * w * d[e];
+                }
             }
-            if (p.stored && t < a.L) {
-                store_channels<T, NARROW>(du + (int64_t)t * a.dus.step, a.D, rounded4<T>(gu));
-                store_channels<T, NARROW>(dgate + (int64_t)t * a.dgs.step, a.D, rounded4<T>(gz));
-            }
-        }
-        if (t0 == 0 && a.dh0 && p.stored) store_channels<float, NARROW>(a.dh0 + state, a.D, back);
+        });
+        store_steps<T, NARROW>(d, a.du, a.dus, p, t0, a.L, full);
+        store_steps<T, NARROW>(u, a.dgate, a.dgs, p, t0, a.L, full);
+        if (t0 == 0 && a.dh0 && p.stored) store_channels<float, NARROW>(a.dh0 + state, back);
         if (!LOOK && tb > 0) {
             if (p.row == 0) s_end[p.vec] = back;
             __syncthreads();
@@ -449,13 +476,14 @@ __global__ void __launch_bounds__(256) gated_step_kernel(const T *__restrict__ g
 
 // Vectors of channels and threads along time of a workgroup, sequences per workgroup, chunks of a sequence; look: a workgroup per chunk.
 struct GatedPlan { int lgcx, lgspan, rows, seqs, threads, nCX, nTB; bool look; int64_t blocks; size_t ticket_bytes, desc_bytes; };
-GatedPlan plan_gated(int64_t Bt, int64_t L, int64_t D)
+GatedPlan plan_gated(int64_t Bt, int64_t L, int64_t D, int dtype)
 {
     GatedPlan pl{};
+    const int full_line = dtype == SSM_F32 ? 4 : 5;          // log2 of the vectors of a 128-byte line
     const int64_t vecs = (D + GV - 1) / GV, rows = (L + GE - 1) / GE;
     const auto blocks_at = [&](int lg) { return Bt * ((vecs + (1 << lg) - 1) >> lg); };
     pl.lgcx = 0;
-    while (pl.lgcx < 4 && (1 << pl.lgcx) < vecs) ++pl.lgcx;
+    while (pl.lgcx < full_line && (1 << pl.lgcx) < vecs) ++pl.lgcx;
     const int widest = pl.lgcx;
     while (pl.lgcx > 2 && rows > (GATED_MAX_THREADS >> pl.lgcx) && blocks_at(pl.lgcx) < 512) --pl.lgcx;
     if (rows > (GATED_MAX_THREADS >> pl.lgcx)) pl.lgcx = widest;
@@ -510,7 +538,7 @@ ssm_status check_shape(int dtype, int64_t Bt, int64_t L, int64_t D)
 
 ssm_status launch_gated(GatedArgs &a, bool reverse, int dtype, int linear, void *workspace, size_t ws_bytes, hipStream_t s)
 {
-    const GatedPlan pl = plan_gated(a.Bt, a.L, a.D);
+    const GatedPlan pl = plan_gated(a.Bt, a.L, a.D, dtype);
     if (pl.blocks > 0x7fffffffLL) return SSM_ERR_UNSUPPORTED;
     a.lgcx = pl.lgcx; a.lgspan = pl.lgspan; a.rows = pl.rows; a.seqs = pl.seqs; a.nCX = pl.nCX; a.nTB = pl.nTB;
     a.carry_rows = (int)ssm_gated_carry_rows(a.L);
@@ -553,7 +581,7 @@ int64_t ssm_gated_carry_rows(int64_t L) { return L > 0 ? (L - 1) / SSM_GATED_CAR
 size_t ssm_gated_workspace_bytes(int64_t Bt, int64_t L, int64_t D, int dtype, int)
 {
     if (check_shape(dtype, Bt, L, D) != SSM_OK) return 0;
-    const GatedPlan pl = plan_gated(Bt, L, D);
+    const GatedPlan pl = plan_gated(Bt, L, D, dtype);
     return pl.look ? GATED_HEADER + pl.ticket_bytes + pl.desc_bytes : 0;
 }
 
