@@ -19,7 +19,7 @@ inline bool misaligned(const void *p, size_t a) { return (reinterpret_cast<uintp
 
 constexpr int GE = 8;                        // consecutive steps of a thread
 constexpr int GV = 2;                        // neighbouring channels of a thread
-constexpr int GATED_MAX_THREADS = 512, GATED_MAX_VECS = 32;
+constexpr int GATED_MAX_THREADS = 1024, GATED_MAX_VECS = 32;
 struct GatedArgs {
     const void *gate, *u, *dh;
     ssm_strides gs, us, dhs;
@@ -34,10 +34,11 @@ struct GatedArgs {
     int rows, seqs;                          // threads along time of a sequence, sequences of a workgroup (several: each within a wavefront)
     int nCX, nTB, carry_rows;                // channel blocks, chunks along time
     // chunks in workgroups of their own
-    unsigned long long *desc;                // [nTB][nCX * Bt][3][64] tagged words, zero on entry: A, S and the state behind the chunk
+    unsigned long long *desc;                // [nTB][chains][3][64] tagged words, zero on entry: A, S and the state behind the chunk
     uint32_t *ticket, *err;
     uint32_t spin_limit;
-    FastDiv by_chains;                       // nCX * Bt
+    int chains, per_xcd;                     // chains: channel blocks of sequences (of groups of sequences); of them in an XCD
+    FastDiv by_round;                        // 8 * per_xcd
 };
 constexpr int GATED_DESC_WORDS = 3 * 64;
 
@@ -152,9 +153,9 @@ __device__ __forceinline__ void publish2(unsigned long long *w, f32x2 v, unsigne
 // UP: rows in the order of time.  `chunk`: number along the direction of the scan; `total`: the chunk's map, valid where `ends`; v0: what flows into the first chunk.
 template <bool UP> __device__ __forceinline__ f32x2 look_back(const GatedArgs &a, const Place &p, MapLds &lds, f32x2 *s_base, int chunk, int chain, const Map &total, bool ends, f32x2 v0)
 {
-    const int cx = 1 << a.lgcx, chains = a.nCX * a.Bt, group = chunk / a.rows * a.rows, row = UP ? p.row : a.rows - 1 - p.row;
-    unsigned long long *mine = a.desc + ((int64_t)chunk * chains + chain) * GATED_DESC_WORDS + p.vec * GV;
-    const int64_t back = (int64_t)chains * GATED_DESC_WORDS;
+    const int cx = 1 << a.lgcx, group = chunk / a.rows * a.rows, row = UP ? p.row : a.rows - 1 - p.row;
+    unsigned long long *mine = a.desc + ((int64_t)chunk * a.chains + chain) * GATED_DESC_WORDS + p.vec * GV;
+    const int64_t back = (int64_t)a.chains * GATED_DESC_WORDS;
     if (ends && chunk + 1 < a.nTB) {
         publish2(mine, total.A, 1);
         publish2(mine + 64, total.S, total.r ? 2 : 1);
@@ -185,12 +186,13 @@ template <bool UP> __device__ __forceinline__ f32x2 look_back(const GatedArgs &a
     if (ends && chunk + 1 < a.nTB && (chunk + 1) % a.rows == 0) publish2(mine + 128, apply(total, v), 3);
     return v;
 }
-// the chunk and the chain of this workgroup
-__device__ __forceinline__ int take_ticket(const GatedArgs &a, int &chain)
+// Workgroups go to the eight XCDs in turn.  Neighbouring channel blocks share cache lines where rows are not whole lines (or a block is not), so
+// neighbouring chains go to one XCD, whose L2 puts the pieces of a line together.  The chain of workgroup n of a round, or one past the last.
+__device__ __forceinline__ int chain_of(const GatedArgs &a, int n) { return (n & 7) * a.per_xcd + (n >> 3); }
+// the chunk of this workgroup, of those of its chain in the order in which they start
+__device__ __forceinline__ int take_ticket(const GatedArgs &a, int chain)
 {
     __shared__ int s_chunk;
-    const int chains = a.nCX * a.Bt;
-    chain = (int)blockIdx.x - (int)a.by_chains(blockIdx.x) * chains;
     if (threadIdx.x == 0) s_chunk = (int)atomicAdd(a.ticket + (int64_t)chain * SCAN_TICKET_STRIDE, 1u);
     __syncthreads();
     return __builtin_amdgcn_readfirstlane(s_chunk);
@@ -284,7 +286,9 @@ __global__ void __launch_bounds__(GATED_MAX_THREADS) gated_fwd_kernel(GatedArgs 
 {
     __shared__ MapLds lds;
     __shared__ f32x2 s_end[GATED_MAX_VECS];  // state at the end of the chunk before
-    int chain = blockIdx.x, first = 0;
+    const int chain = chain_of(a, LOOK ? (int)(blockIdx.x - a.by_round(blockIdx.x) * 8u * a.per_xcd) : (int)blockIdx.x);
+    if (chain >= a.chains) return;
+    int first = 0;
     if constexpr (LOOK) first = take_ticket(a, chain);
     const Place p(a, chain);
     const int cx = 1 << a.lgcx, steps = GE * a.rows;
@@ -350,11 +354,13 @@ __global__ void __launch_bounds__(GATED_MAX_THREADS) gated_fwd_kernel(GatedArgs 
 }
 
 template <class T, bool LINEAR, bool NARROW, bool LOOK>
-__global__ void __launch_bounds__(GATED_MAX_THREADS, 4) gated_bwd_kernel(GatedArgs a)
+__global__ void __launch_bounds__(GATED_MAX_THREADS) gated_bwd_kernel(GatedArgs a)
 {
     __shared__ MapLds lds_up, lds_down;
     __shared__ f32x2 s_end[GATED_MAX_VECS];
-    int chain = blockIdx.x, first = a.nTB - 1;
+    const int chain = chain_of(a, LOOK ? (int)(blockIdx.x - a.by_round(blockIdx.x) * 8u * a.per_xcd) : (int)blockIdx.x);
+    if (chain >= a.chains) return;
+    int first = a.nTB - 1;
     if constexpr (LOOK) first = a.nTB - 1 - take_ticket(a, chain);
     Place p(a, chain);
     const int cx = 1 << a.lgcx, steps = GE * a.rows;
@@ -475,18 +481,19 @@ __global__ void __launch_bounds__(256) gated_step_kernel(const T *__restrict__ g
 }
 
 // Vectors of channels and threads along time of a workgroup, sequences per workgroup, chunks of a sequence; look: a workgroup per chunk.
-struct GatedPlan { int lgcx, lgspan, rows, seqs, threads, nCX, nTB; bool look; int64_t blocks; size_t ticket_bytes, desc_bytes; };
-GatedPlan plan_gated(int64_t Bt, int64_t L, int64_t D, int dtype)
+struct GatedPlan { int lgcx, lgspan, rows, seqs, threads, nCX, nTB; bool look; int64_t chains, blocks; size_t ticket_bytes, desc_bytes; };
+GatedPlan plan_gated(int64_t Bt, int64_t L, int64_t D)
 {
     GatedPlan pl{};
-    const int full_line = dtype == SSM_F32 ? 4 : 5;          // log2 of the vectors of a 128-byte line
     const int64_t vecs = (D + GV - 1) / GV, rows = (L + GE - 1) / GE;
-    const auto blocks_at = [&](int lg) { return Bt * ((vecs + (1 << lg) - 1) >> lg); };
-    pl.lgcx = 0;
-    while (pl.lgcx < full_line && (1 << pl.lgcx) < vecs) ++pl.lgcx;
-    const int widest = pl.lgcx;
-    while (pl.lgcx > 2 && rows > (GATED_MAX_THREADS >> pl.lgcx) && blocks_at(pl.lgcx) < 512) --pl.lgcx;
-    if (rows > (GATED_MAX_THREADS >> pl.lgcx)) pl.lgcx = widest;
+    while (pl.lgcx < 5 && (1 << pl.lgcx) < vecs) ++pl.lgcx;
+    int most = 512 >> pl.lgcx;               // threads along time
+    const auto chains_at = [&](int lg) { return Bt * ((vecs + (1 << lg) - 1) >> lg); };
+    const bool few = chains_at(pl.lgcx) < 256;
+    if (rows > most && few && rows << (pl.lgcx < 4 ? pl.lgcx : 4) <= GATED_MAX_THREADS) {
+        if (pl.lgcx > 4) pl.lgcx = 4;
+        most = GATED_MAX_THREADS >> pl.lgcx;
+    }
     const int cx = 1 << pl.lgcx;
     if (rows * cx <= 64) {                   // a sequence within a wavefront
         pl.lgspan = pl.lgcx;
@@ -497,7 +504,7 @@ GatedPlan plan_gated(int64_t Bt, int64_t L, int64_t D, int dtype)
         pl.seqs = pl.threads >> pl.lgspan;
         pl.nTB = 1;
     } else {                                 // a sequence, or a chunk of one, per workgroup: whole wavefronts
-        const int per_wave = 64 >> pl.lgcx, most = GATED_MAX_THREADS >> pl.lgcx;
+        const int per_wave = 64 >> pl.lgcx;
         pl.lgspan = 6;
         pl.rows = (int)(rows <= most ? (rows + per_wave - 1) / per_wave * per_wave : most);
         pl.threads = pl.rows * cx;
@@ -505,12 +512,12 @@ GatedPlan plan_gated(int64_t Bt, int64_t L, int64_t D, int dtype)
         pl.nTB = (int)((rows + pl.rows - 1) / pl.rows);
     }
     pl.nCX = (int)((vecs + cx - 1) >> pl.lgcx);
-    const int64_t chains = (int64_t)pl.nCX * ((Bt + pl.seqs - 1) / pl.seqs);
-    pl.look = pl.nTB > 1 && chains < 512 && chains * pl.nTB <= 0x7fffffffLL;
-    pl.blocks = pl.look ? chains * pl.nTB : chains;
+    pl.chains = (int64_t)pl.nCX * ((Bt + pl.seqs - 1) / pl.seqs);
+    pl.look = pl.nTB > 1 && few;
+    pl.blocks = (pl.chains + 7) / 8 * 8 * (pl.look ? pl.nTB : 1);
     if (pl.look) {
-        pl.ticket_bytes = (size_t)chains * SCAN_TICKET_STRIDE * sizeof(uint32_t);
-        pl.desc_bytes = (size_t)pl.blocks * GATED_DESC_WORDS * sizeof(unsigned long long);
+        pl.ticket_bytes = (size_t)pl.chains * SCAN_TICKET_STRIDE * sizeof(uint32_t);
+        pl.desc_bytes = (size_t)pl.chains * pl.nTB * GATED_DESC_WORDS * sizeof(unsigned long long);
     }
     return pl;
 }
@@ -538,10 +545,12 @@ ssm_status check_shape(int dtype, int64_t Bt, int64_t L, int64_t D)
 
 ssm_status launch_gated(GatedArgs &a, bool reverse, int dtype, int linear, void *workspace, size_t ws_bytes, hipStream_t s)
 {
-    const GatedPlan pl = plan_gated(a.Bt, a.L, a.D, dtype);
+    const GatedPlan pl = plan_gated(a.Bt, a.L, a.D);
     if (pl.blocks > 0x7fffffffLL) return SSM_ERR_UNSUPPORTED;
     a.lgcx = pl.lgcx; a.lgspan = pl.lgspan; a.rows = pl.rows; a.seqs = pl.seqs; a.nCX = pl.nCX; a.nTB = pl.nTB;
     a.carry_rows = (int)ssm_gated_carry_rows(a.L);
+    a.chains = (int)pl.chains; a.per_xcd = (int)((pl.chains + 7) / 8);
+    a.by_round = FastDiv::by(8u * (unsigned)a.per_xcd);
     if (pl.look) {
         const size_t scratch = pl.ticket_bytes + pl.desc_bytes;
         if (!workspace || misaligned(workspace, 256) || ws_bytes < GATED_HEADER + scratch) return SSM_ERR_WORKSPACE;
@@ -550,7 +559,6 @@ ssm_status launch_gated(GatedArgs &a, bool reverse, int dtype, int linear, void 
         a.ticket = reinterpret_cast<uint32_t *>(ws + GATED_HEADER);
         a.desc = reinterpret_cast<unsigned long long *>(ws + GATED_HEADER + pl.ticket_bytes);
         a.spin_limit = scan_spin_limit();
-        a.by_chains = FastDiv::by((unsigned)((int64_t)pl.nCX * a.Bt));
         if (launch_clear(reinterpret_cast<WsHeader *>(ws), ws + GATED_HEADER, scratch, s) != hipSuccess) return SSM_ERR_HIP;
     }
     const dim3 grid((unsigned)pl.blocks), block((unsigned)pl.threads);
@@ -581,7 +589,7 @@ int64_t ssm_gated_carry_rows(int64_t L) { return L > 0 ? (L - 1) / SSM_GATED_CAR
 size_t ssm_gated_workspace_bytes(int64_t Bt, int64_t L, int64_t D, int dtype, int)
 {
     if (check_shape(dtype, Bt, L, D) != SSM_OK) return 0;
-    const GatedPlan pl = plan_gated(Bt, L, D, dtype);
+    const GatedPlan pl = plan_gated(Bt, L, D);
     return pl.look ? GATED_HEADER + pl.ticket_bytes + pl.desc_bytes : 0;
 }
 
