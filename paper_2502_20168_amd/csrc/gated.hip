@@ -34,13 +34,14 @@ struct GatedArgs {
     int rows, seqs;                          // threads along time of a sequence, sequences of a workgroup (several: each within a wavefront)
     int nCX, nTB, carry_rows;                // channel blocks, chunks along time
     // chunks in workgroups of their own
-    unsigned long long *desc;                // [nTB][chains][3][64] tagged words, zero on entry: A, S and the state behind the chunk
+    unsigned long long *desc;                // [nTB][chains][5][64] tagged words, zero on entry
     uint32_t *ticket, *err;
+    int groups;                              // of a block
     uint32_t spin_limit;
-    int chains, per_xcd;                     // chains: channel blocks of sequences (of groups of sequences); of them in an XCD
-    FastDiv by_round;                        // 8 * per_xcd
+    int chains, per_xcd;                     // chains: channel blocks of sequences (of groups of sequences); of them in an XCD, 0: in turn
+    int round; FastDiv by_round;             // workgroups per chunk of all chains
 };
-constexpr int GATED_DESC_WORDS = 3 * 64;
+constexpr int GATED_DESC_WORDS = 5 * 64;
 
 // sigmoid(z) and 1 - sigmoid(z), both to the relative precision of the exponential: the difference where it is at least a half, exp(-z) sigmoid(z) else.
 struct Gate { float f, i; };
@@ -130,9 +131,14 @@ struct Place {
     }
 };
 
-// What a chunk's neighbours hand over where every chunk has a workgroup of its own.  A workgroup publishes the map of its chunk before it waits for anything; then
-// each of its rows fetches the map of one earlier chunk of its group of `rows` chunks, all at once, and one row the state behind the last chunk of
-// the group before.  The order of the compositions is fixed, whatever the timing: results are repeatable.  Chunks are numbered by a ticket per chain (the chunks of one
+// What a chunk's neighbours hand over where every chunk has a workgroup of its own.  With R threads along time to a workgroup, R chunks are a group and `groups` groups a
+// block.  A workgroup publishes the map of its chunk before it waits for anything; then each of its rows fetches the map of one earlier chunk of
+// its group, all at once.  With several groups to a block the last workgroup of a group publishes the map of the group, and each row fetches that of one earlier group of the
+// block; one row fetches the state behind the block before.  R groups to a block, and the state reaches every chunk in two trips up to R^2 chunks (256: 32768
+// steps); one, and it goes from group to group.  That costs less for two groups, and where the grid takes several rounds and the groups before have long ended:
+// forward and gradient of 16 x 4096 x 512 bf16 56 and 93 us, with R groups 63 and 99; of 1 x 16384 x 256 f32 21.9 and 26.4, with R groups 19.6 and 25.1; of
+// 1 x 60000 x 64 40.8 and 42.2, with R groups 24.7 and 27.5.
+// The order of the compositions is fixed, whatever the timing: results are repeatable.  Chunks are numbered by a ticket per chain (the chunks of one
 // sequence and channel block), so that a workgroup waits for such as have started; a wait that gives up hands on NaN and says so in the workspace.
 __device__ __forceinline__ bool wait_words(const unsigned long long *w, unsigned limit, f32x2 &v, unsigned &tag)
 {
@@ -150,45 +156,58 @@ __device__ __forceinline__ void publish2(unsigned long long *w, f32x2 v, unsigne
     publish_word(w, v[0], tag);
     publish_word(w + 1, v[1], tag);
 }
+// the map at w, or one to NaN
+__device__ __forceinline__ Map wait_map(const GatedArgs &a, const unsigned long long *w)
+{
+    Map m;
+    unsigned tag;
+    const bool got = wait_words(w, a.spin_limit, m.A, tag) && wait_words(w + 64, a.spin_limit, m.S, tag);
+    m.r = tag == 2;
+    if (!got) { atomicOr(a.err, 1u); m = {f32x2{0.f, 0.f}, f32x2{__builtin_nanf(""), __builtin_nanf("")}, 1}; }
+    return m;
+}
+__device__ __forceinline__ void publish_map(unsigned long long *w, const Map &m)
+{
+    publish2(w, m.A, 1);
+    publish2(w + 64, m.S, m.r ? 2 : 1);
+}
+// one map per row and vector of channels -> their composition, the first row's first
+template <bool UP> __device__ __forceinline__ Map compose_rows(const Place &p, MapLds &lds, Map m, int cx)
+{
+    m = inclusive_in_wave<UP, true>(m, p.lane, cx, p.span);
+    __syncthreads();                         // (what was in lds has been read)
+    if (UP ? p.lane >= 64 - cx : p.lane < cx) put(lds, p.wave, p.vec, m);
+    __syncthreads();
+    return fold<UP>(lds, p.vec, p.waves, p.waves);
+}
 // UP: rows in the order of time.  `chunk`: number along the direction of the scan; `total`: the chunk's map, valid where `ends`; v0: what flows into the first chunk.
+// Words of a chunk: its map [0, 128), the state behind the block that it ends [128, 192), the map of the group that it ends [192, 320).
 template <bool UP> __device__ __forceinline__ f32x2 look_back(const GatedArgs &a, const Place &p, MapLds &lds, f32x2 *s_base, int chunk, int chain, const Map &total, bool ends, f32x2 v0)
 {
-    const int cx = 1 << a.lgcx, group = chunk / a.rows * a.rows, row = UP ? p.row : a.rows - 1 - p.row;
+    const int cx = 1 << a.lgcx, R = a.rows, RB = R * a.groups, group = chunk / R * R, block = chunk / RB * RB, row = UP ? p.row : R - 1 - p.row;
     unsigned long long *mine = a.desc + ((int64_t)chunk * a.chains + chain) * GATED_DESC_WORDS + p.vec * GV;
     const int64_t back = (int64_t)a.chains * GATED_DESC_WORDS;
-    if (ends && chunk + 1 < a.nTB) {
-        publish2(mine, total.A, 1);
-        publish2(mine + 64, total.S, total.r ? 2 : 1);
+    const bool more = chunk + 1 < a.nTB;
+    if (ends && more) publish_map(mine, total);
+    Map chunks = identity(), groups = identity();
+    if (chunk > group) chunks = compose_rows<UP>(p, lds, group + row < chunk ? wait_map(a, mine - (chunk - group - row) * back) : identity(), cx);
+    if (ends && more && a.groups > 1 && (chunk + 1) % R == 0) publish_map(mine + 192, after<true>(total, chunks));
+    if (block > 0 && row == 0) {
+        unsigned tag;
+        f32x2 base;
+        if (!wait_words(mine - (chunk - block + 1) * back + 128, a.spin_limit, base, tag)) { atomicOr(a.err, 1u); base = f32x2{__builtin_nanf(""), __builtin_nanf("")}; }
+        s_base[p.vec] = base;
     }
-    f32x2 v = v0;
-    if (chunk > 0) {                         // (uniform)
-        const f32x2 nan = {__builtin_nanf(""), __builtin_nanf("")};
-        Map m = identity();
-        if (group + row < chunk) {
-            const unsigned long long *w = mine - (chunk - group - row) * back;
-            unsigned tag;
-            const bool got = wait_words(w, a.spin_limit, m.A, tag) && wait_words(w + 64, a.spin_limit, m.S, tag);
-            m.r = tag == 2;
-            if (!got) { atomicOr(a.err, 1u); m.S = nan; m.r = 1; }
-        }
-        if (group > 0 && row == 0) {
-            unsigned tag;
-            f32x2 base;
-            if (!wait_words(mine - (chunk - group + 1) * back + 128, a.spin_limit, base, tag)) { atomicOr(a.err, 1u); base = nan; }
-            s_base[p.vec] = base;
-        }
-        m = inclusive_in_wave<UP, true>(m, p.lane, cx, p.span);
-        __syncthreads();                     // (the maps of the chunk itself have been read)
-        if (UP ? p.lane >= 64 - cx : p.lane < cx) put(lds, p.wave, p.vec, m);
-        __syncthreads();
-        v = apply(fold<UP>(lds, p.vec, p.waves, p.waves), group > 0 ? s_base[p.vec] : v0);
-    }
-    if (ends && chunk + 1 < a.nTB && (chunk + 1) % a.rows == 0) publish2(mine + 128, apply(total, v), 3);
+    if (group > block) groups = compose_rows<UP>(p, lds, block + row * R < group ? wait_map(a, mine - (chunk - block - row * R - R + 1) * back + 192) : identity(), cx);
+    else if (block > 0) __syncthreads();
+    const f32x2 v = apply(chunks, apply(groups, block > 0 ? s_base[p.vec] : v0));
+    if (ends && more && (chunk + 1) % RB == 0) publish2(mine + 128, apply(total, v), 3);
     return v;
 }
 // Workgroups go to the eight XCDs in turn.  Neighbouring channel blocks share cache lines where rows are not whole lines (or a block is not), so
-// neighbouring chains go to one XCD, whose L2 puts the pieces of a line together.  The chain of workgroup n of a round, or one past the last.
-__device__ __forceinline__ int chain_of(const GatedArgs &a, int n) { return (n & 7) * a.per_xcd + (n >> 3); }
+// neighbouring chains go to one XCD, whose L2 puts the pieces of a line together (64 x 1000 x 300 f32 forward 58 -> 47 us, bf16 gradient 68 -> 55; where rows are whole
+// lines no difference).  Not with fewer than 64 chains, which would leave XCDs idle.  The chain of workgroup n of a round, or one past the last.
+__device__ __forceinline__ int chain_of(const GatedArgs &a, int n) { return a.per_xcd ? (n & 7) * a.per_xcd + (n >> 3) : n; }
 // the chunk of this workgroup, of those of its chain in the order in which they start
 __device__ __forceinline__ int take_ticket(const GatedArgs &a, int chain)
 {
@@ -286,7 +305,7 @@ __global__ void __launch_bounds__(GATED_MAX_THREADS) gated_fwd_kernel(GatedArgs 
 {
     __shared__ MapLds lds;
     __shared__ f32x2 s_end[GATED_MAX_VECS];  // state at the end of the chunk before
-    const int chain = chain_of(a, LOOK ? (int)(blockIdx.x - a.by_round(blockIdx.x) * 8u * a.per_xcd) : (int)blockIdx.x);
+    const int chain = chain_of(a, LOOK ? (int)(blockIdx.x - a.by_round(blockIdx.x) * (unsigned)a.round) : (int)blockIdx.x);
     if (chain >= a.chains) return;
     int first = 0;
     if constexpr (LOOK) first = take_ticket(a, chain);
@@ -358,7 +377,7 @@ __global__ void __launch_bounds__(GATED_MAX_THREADS) gated_bwd_kernel(GatedArgs 
 {
     __shared__ MapLds lds_up, lds_down;
     __shared__ f32x2 s_end[GATED_MAX_VECS];
-    const int chain = chain_of(a, LOOK ? (int)(blockIdx.x - a.by_round(blockIdx.x) * 8u * a.per_xcd) : (int)blockIdx.x);
+    const int chain = chain_of(a, LOOK ? (int)(blockIdx.x - a.by_round(blockIdx.x) * (unsigned)a.round) : (int)blockIdx.x);
     if (chain >= a.chains) return;
     int first = a.nTB - 1;
     if constexpr (LOOK) first = a.nTB - 1 - take_ticket(a, chain);
@@ -481,7 +500,7 @@ __global__ void __launch_bounds__(256) gated_step_kernel(const T *__restrict__ g
 }
 
 // Vectors of channels and threads along time of a workgroup, sequences per workgroup, chunks of a sequence; look: a workgroup per chunk.
-struct GatedPlan { int lgcx, lgspan, rows, seqs, threads, nCX, nTB; bool look; int64_t chains, blocks; size_t ticket_bytes, desc_bytes; };
+struct GatedPlan { int lgcx, lgspan, rows, seqs, threads, nCX, nTB; bool look; int per_xcd; int64_t chains, round, blocks; size_t ticket_bytes, desc_bytes; };
 GatedPlan plan_gated(int64_t Bt, int64_t L, int64_t D)
 {
     GatedPlan pl{};
@@ -514,7 +533,9 @@ GatedPlan plan_gated(int64_t Bt, int64_t L, int64_t D)
     pl.nCX = (int)((vecs + cx - 1) >> pl.lgcx);
     pl.chains = (int64_t)pl.nCX * ((Bt + pl.seqs - 1) / pl.seqs);
     pl.look = pl.nTB > 1 && few;
-    pl.blocks = (pl.chains + 7) / 8 * 8 * (pl.look ? pl.nTB : 1);
+    pl.per_xcd = pl.chains >= 64 ? (int)((pl.chains + 7) / 8) : 0;
+    pl.round = pl.per_xcd ? 8 * (int64_t)pl.per_xcd : pl.chains;
+    pl.blocks = pl.round * (pl.look ? pl.nTB : 1);
     if (pl.look) {
         pl.ticket_bytes = (size_t)pl.chains * SCAN_TICKET_STRIDE * sizeof(uint32_t);
         pl.desc_bytes = (size_t)pl.chains * pl.nTB * GATED_DESC_WORDS * sizeof(unsigned long long);
@@ -549,8 +570,8 @@ ssm_status launch_gated(GatedArgs &a, bool reverse, int dtype, int linear, void 
     if (pl.blocks > 0x7fffffffLL) return SSM_ERR_UNSUPPORTED;
     a.lgcx = pl.lgcx; a.lgspan = pl.lgspan; a.rows = pl.rows; a.seqs = pl.seqs; a.nCX = pl.nCX; a.nTB = pl.nTB;
     a.carry_rows = (int)ssm_gated_carry_rows(a.L);
-    a.chains = (int)pl.chains; a.per_xcd = (int)((pl.chains + 7) / 8);
-    a.by_round = FastDiv::by(8u * (unsigned)a.per_xcd);
+    a.chains = (int)pl.chains; a.per_xcd = pl.per_xcd; a.round = (int)pl.round;
+    a.by_round = FastDiv::by((unsigned)a.round);
     if (pl.look) {
         const size_t scratch = pl.ticket_bytes + pl.desc_bytes;
         if (!workspace || misaligned(workspace, 256) || ws_bytes < GATED_HEADER + scratch) return SSM_ERR_WORKSPACE;
@@ -559,6 +580,7 @@ ssm_status launch_gated(GatedArgs &a, bool reverse, int dtype, int linear, void 
         a.ticket = reinterpret_cast<uint32_t *>(ws + GATED_HEADER);
         a.desc = reinterpret_cast<unsigned long long *>(ws + GATED_HEADER + pl.ticket_bytes);
         a.spin_limit = scan_spin_limit();
+        a.groups = pl.blocks <= 1024 && pl.nTB > 2 * pl.rows ? pl.rows : 1;          // (up to about two rounds, three groups and more)
         if (launch_clear(reinterpret_cast<WsHeader *>(ws), ws + GATED_HEADER, scratch, s) != hipSuccess) return SSM_ERR_HIP;
     }
     const dim3 grid((unsigned)pl.blocks), block((unsigned)pl.threads);

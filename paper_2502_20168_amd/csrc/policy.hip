@@ -26,7 +26,7 @@ struct PolicyArgs {
     float *logp, *entropy, *lse;             // written by the forward pass, read by the gradient pass on its own
     const float *dloss;
     void *dlogits; int64_t dpitch;
-    float *row_loss;                         // [N] weighted
+    float *part_loss;                        // weighted, of every workgroup's row or every wavefront's rows
     float mean_weight;                       // of a row where none are given
 };
 
@@ -160,14 +160,14 @@ template <class T> __device__ __forceinline__ typename Unit<T>::wide gradient(ty
     return r;
 }
 
-// The end of a row's statistics: its results (stored by one lane) and what its gradient needs.
-__device__ __forceinline__ Slope finish_row(const PolicyArgs &a, int64_t n, const Row &r, const Sums &q, float xa, bool store)
+// The end of a row's statistics: its results (stored by one lane), its weighted loss and what its gradient needs.
+__device__ __forceinline__ Slope finish_row(const PolicyArgs &a, int64_t n, const Row &r, const Sums &q, float xa, bool store, float &loss)
 {
     const bool idle = r.idle || q.s == 0.f;
     const double ls = log((double)q.s), entropy = ls - (double)q.t * 0.6931471805599453 / (double)q.s, logp = ((double)xa - (double)q.m) - ls;
     const Terms t = row_terms(a, r, logp, entropy);
+    loss = idle ? 0.f : (float)((double)r.weight * t.loss);
     if (store) {
-        a.row_loss[n] = idle ? 0.f : (float)((double)r.weight * t.loss);
         a.logp[n] = idle ? 0.f : (float)logp;
         a.entropy[n] = idle ? 0.f : (float)entropy;
         a.lse[n] = idle ? -INFINITY : (float)((double)q.m + ls);
@@ -221,7 +221,11 @@ __global__ void __launch_bounds__(256) policy_wave_kernel(PolicyArgs a, int lane
         for (int j = 0; j < U; ++j) add_unit<T>(v[j], q.m, q.s, q.t);
         for (int o = 1; o < width; o <<= 1) { q.s += __shfl_xor(q.s, o); q.t += __shfl_xor(q.t, o); }
         stay_packed<T>(v);
-        g = finish_row(a, n, r, q, xa, sub == 0 && want < a.N);
+        const bool mine = sub == 0 && want < a.N;
+        float loss;
+        g = finish_row(a, n, r, q, xa, mine, loss);
+        loss = wave_sum(mine ? loss : 0.f);
+        if (lane == 0) a.part_loss[(int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)] = loss;
     } else {
         g = stored_row(a, n, r, xa);
     }
@@ -268,8 +272,9 @@ __global__ void __launch_bounds__(1024) policy_row_kernel(PolicyArgs a)
     T *dx = GRAD ? static_cast<T *>(a.dlogits) + n * a.dpitch : nullptr;
     typename Unit<T>::raw v[U];
     Slope g;
+    float loss;
     if (r.idle) {                            // (uniform)
-        g = finish_row(a, n, r, Sums{0.f, 0.f, 0.f}, 0.f, tid == 0);
+        g = finish_row(a, n, r, Sums{0.f, 0.f, 0.f}, 0.f, tid == 0, loss);
 #pragma unroll
         for (int j = 0; j < U; ++j) {
 #pragma unroll
@@ -288,8 +293,9 @@ __global__ void __launch_bounds__(1024) policy_row_kernel(PolicyArgs a)
         for (int j = 0; j < U; ++j) add_unit<T>(v[j], q.m, q.s, q.t);
         stay_packed<T>(v);
         row_sums(lds, q, waves);             // (behind its barrier the gradient may be stored over the logits)
-        g = finish_row(a, n, r, q, xa, tid == 0);
+        g = finish_row(a, n, r, q, xa, tid == 0, loss);
     }
+    if (tid == 0) a.part_loss[n] = loss;
     if constexpr (GRAD) {
 #pragma unroll
         for (int j = 0; j < U; ++j) {
@@ -326,7 +332,9 @@ __global__ void __launch_bounds__(1024) policy_stream_kernel(PolicyArgs a)
             q = {m, q.s * scale, scale * fmaf(q.s, d, q.t)};
             row_sums(lds, q, waves);
         }
-        g = finish_row(a, n, r, q, xa, tid == 0);
+        float loss;
+        g = finish_row(a, n, r, q, xa, tid == 0, loss);
+        if (tid == 0) a.part_loss[n] = loss;
     } else {
         __syncthreads();                     // every thread has read the action's logit before the first one stores over it
         g = stored_row(a, n, r, xa);
@@ -343,18 +351,27 @@ __global__ void __launch_bounds__(1024) policy_stream_kernel(PolicyArgs a)
     }
 }
 
-// loss = sum of the rows', in one fixed order
-__global__ void __launch_bounds__(1024) policy_sum_kernel(const float *__restrict__ row_loss, int64_t n, float *__restrict__ loss)
+// loss = sum of the parts, in one fixed order
+__global__ void __launch_bounds__(1024) policy_sum_kernel(const float *__restrict__ part, int64_t n, float *__restrict__ loss)
 {
     __shared__ double red[16];
     double s = 0.0;
-    for (int64_t i = threadIdx.x; i < n; i += 1024) s += (double)row_loss[i];
+    int64_t i = threadIdx.x;
+    const int64_t step = blockDim.x;
+    for (; i + 7 * step < n; i += 8 * step) {
+        float v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = part[i + k * step];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s += (double)v[k];
+    }
+    for (; i < n; i += step) s += (double)part[i];
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int i = 1; i < 16; ++i) s += red[i];
+        for (int k = 1; k < (int)blockDim.x >> 6; ++k) s += red[k];
         loss[0] = (float)s;
     }
 }
@@ -378,19 +395,17 @@ ssm_status check_gradient(const PolicyArgs &a, int dtype, int64_t N, int64_t K)
     return N > 1 && a.dpitch > SSM_MAX_ELEMS / N ? SSM_ERR_UNSUPPORTED : SSM_OK;
 }
 
-ssm_status launch_sum(const PolicyArgs &a, float *loss, hipStream_t s)
-{
-    hipLaunchKernelGGL(policy_sum_kernel, dim3(1), dim3(1024), 0, s, a.row_loss, a.N, loss);
-    return hipGetLastError() == hipSuccess ? SSM_OK : SSM_ERR_HIP;
-}
 // Who holds a row: part of a wavefront, a wavefront, a workgroup, or nobody.
-template <class T, bool STATS, bool GRAD> void launch_rows_of(const PolicyArgs &a, hipStream_t s)
+// Returns the number of parts of the loss.
+template <class T, bool STATS, bool GRAD> int64_t launch_rows_of(const PolicyArgs &a, hipStream_t s)
 {
     constexpr int V = Unit<T>::V;
     const int64_t units = ((int64_t)a.K + V - 1) / V;
     const auto wave = [&](auto u, int lanes) {
         const int64_t rows = 4 * (64 >> lanes);
-        hipLaunchKernelGGL((policy_wave_kernel<T, decltype(u)::value, STATS, GRAD>), dim3((unsigned)((a.N + rows - 1) / rows)), dim3(256), 0, s, a, lanes);
+        const int64_t blocks = (a.N + rows - 1) / rows;
+        hipLaunchKernelGGL((policy_wave_kernel<T, decltype(u)::value, STATS, GRAD>), dim3((unsigned)blocks), dim3(256), 0, s, a, lanes);
+        return 4 * blocks;
     };
     if (units <= 64) {
         int lanes = 0;
@@ -403,6 +418,7 @@ template <class T, bool STATS, bool GRAD> void launch_rows_of(const PolicyArgs &
     if constexpr (STATS) {
         const auto row = [&](auto u, int threads) {
             hipLaunchKernelGGL((policy_row_kernel<T, decltype(u)::value, GRAD>), dim3((unsigned)a.N), dim3(threads), 0, s, a);
+            return a.N;
         };
         if (units <= 256 * 4) return row(std::integral_constant<int, 4>{}, 256);
         if (units <= 256 * 8) return row(std::integral_constant<int, 8>{}, 256);
@@ -411,11 +427,17 @@ template <class T, bool STATS, bool GRAD> void launch_rows_of(const PolicyArgs &
         if (units <= 1024 * 16) return row(std::integral_constant<int, 16>{}, 1024);
     }
     hipLaunchKernelGGL((policy_stream_kernel<T, STATS, GRAD>), dim3((unsigned)a.N), dim3(units <= 2048 ? 256 : 1024), 0, s, a);
+    return a.N;
 }
-template <bool STATS, bool GRAD> ssm_status launch_rows(const PolicyArgs &a, int dtype, hipStream_t s)
+template <bool STATS, bool GRAD> ssm_status launch_rows(const PolicyArgs &a, int dtype, float *loss, hipStream_t s)
 {
-    with_dtype(dtype, [&](auto t) { launch_rows_of<decltype(t), STATS, GRAD>(a, s); });
-    return hipGetLastError() == hipSuccess ? SSM_OK : SSM_ERR_HIP;
+    const int64_t parts = with_dtype(dtype, [&](auto t) { return launch_rows_of<decltype(t), STATS, GRAD>(a, s); });
+    if (hipGetLastError() != hipSuccess) return SSM_ERR_HIP;
+    if constexpr (STATS) {
+        hipLaunchKernelGGL(policy_sum_kernel, dim3(1), dim3(parts <= 256 ? 256 : 1024), 0, s, a.part_loss, parts, loss);
+        if (hipGetLastError() != hipSuccess) return SSM_ERR_HIP;
+    }
+    return SSM_OK;
 }
 
 }  // namespace
@@ -428,7 +450,7 @@ extern "C" {
 size_t ssm_policy_loss_workspace_bytes(int64_t N, int64_t K)
 {
     if (N <= 0 || K <= 0 || N > SSM_MAX_TOKENS || K > (1LL << 30) || K > SSM_MAX_ELEMS / N) return 0;
-    return ((size_t)N * 4 + ALIGN - 1) / ALIGN * ALIGN;
+    return ((size_t)(N + 3) * 4 + ALIGN - 1) / ALIGN * ALIGN;      // (four wavefronts' parts from one row on)
 }
 
 ssm_status ssm_policy_loss_fwd(const void *logits, int64_t pitch, const int64_t *action, const float *logp_old,
@@ -442,8 +464,7 @@ ssm_status ssm_policy_loss_fwd(const void *logits, int64_t pitch, const int64_t 
     if (!loss || misaligned(loss, 4)) return SSM_ERR_INVALID_ARG;
     if (!workspace || misaligned(workspace, ALIGN) || ws_bytes < ssm_policy_loss_workspace_bytes(N, K)) return SSM_ERR_WORKSPACE;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (const ssm_status rc = launch_rows<true, false>(a, dtype, s)) return rc;
-    return launch_sum(a, loss, s);
+    return launch_rows<true, false>(a, dtype, loss, s);
 }
 
 ssm_status ssm_policy_loss_bwd(const void *logits, int64_t pitch, const int64_t *action, const float *logp_old,
@@ -455,7 +476,7 @@ ssm_status ssm_policy_loss_bwd(const void *logits, int64_t pitch, const int64_t 
                  const_cast<float *>(entropy), const_cast<float *>(lse), dloss, dlogits, dpitch, nullptr, N > 0 ? 1.f / (float)N : 0.f};
     if (const ssm_status rc = check_policy(a, dtype, N, K)) return rc;
     if (const ssm_status rc = check_gradient(a, dtype, N, K)) return rc;
-    return launch_rows<false, true>(a, dtype, static_cast<hipStream_t>(stream));
+    return launch_rows<false, true>(a, dtype, nullptr, static_cast<hipStream_t>(stream));
 }
 
 ssm_status ssm_policy_loss_grad(const void *logits, int64_t pitch, const int64_t *action, const float *logp_old,
@@ -470,8 +491,7 @@ ssm_status ssm_policy_loss_grad(const void *logits, int64_t pitch, const int64_t
     if (!loss || misaligned(loss, 4)) return SSM_ERR_INVALID_ARG;
     if (!workspace || misaligned(workspace, ALIGN) || ws_bytes < ssm_policy_loss_workspace_bytes(N, K)) return SSM_ERR_WORKSPACE;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (const ssm_status rc = launch_rows<true, true>(a, dtype, s)) return rc;
-    return launch_sum(a, loss, s);
+    return launch_rows<true, true>(a, dtype, loss, s);
 }
 
 }  // extern "C"

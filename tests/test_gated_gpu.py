@@ -87,6 +87,17 @@ def test_a_long_sequence_of_a_few_channels():
     _compare(_inputs(2, 9000, 24, "bf16", True, "some", True, bias=3.0), "bf16", 5e-5)
 
 
+def test_chunks_groups_and_blocks_of_groups_hand_states_on():
+    """One channel block, 128 steps to a chunk of 16 rows, 16 chunks to a group, 16 groups to a block: a sequence over three blocks, its carries compared with the
+    oracle's states and the gradient with the definition in 64 bits, where resets lie in few places and the state forgets slowly."""
+    import torch
+    L = 2 * 128 * 256 + 5 * 128 * 16 + 3 * 128 + 17
+    s = _inputs(1, L, 64, "f32", False, "none", True, bias=7.0)
+    s["is_first"] = torch.zeros(1, L, dtype=torch.uint8, device="cuda")
+    s["is_first"][0, [40000, 65535, 65536 + 3]] = 1
+    _compare(s, "f32", 1e-4)                 # a state of 1100 steps: a gate near one is good to 2^-24, times the steps it is raised to, times the root of what is added up
+
+
 def test_a_sequence_in_two_parts():
     import torch
     from paper_2502_20168_amd import learn
