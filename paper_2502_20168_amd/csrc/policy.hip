@@ -305,6 +305,34 @@ __global__ void __launch_bounds__(1024) policy_row_kernel(PolicyArgs a)
     }
 }
 
+// Sums over units first .. last - 1 of a row, four of them in flight per thread, over the workgroup (every thread gets the result).  The maximum is the one so far: what
+// was added up under a smaller one is scaled.
+template <class T> __device__ __forceinline__ Sums running_sums(RowLds &lds, const T *x, int first, int last, int K)
+{
+    constexpr int V = Unit<T>::V, U = 4;
+    const int threads = blockDim.x, waves = threads >> 6;
+    const auto under = [](Sums &q, float m) {
+        const float d = fmaxf((q.m - m) * LOG2E, FAR), scale = __builtin_amdgcn_exp2f(d);
+        q = {m, q.s * scale, scale * fmaf(q.s, d, q.t)};
+    };
+    Sums q = {LOWEST, 0.f, 0.f};
+    for (int u = first + (int)threadIdx.x; u < last; u += U * threads) {
+        typename Unit<T>::raw v[U];
+        float m = q.m;
+#pragma unroll
+        for (int j = 0; j < U; ++j) v[j] = load_unit<T>(x, u + j * threads < last ? (u + j * threads) * V : K, K);
+#pragma unroll
+        for (int j = 0; j < U; ++j) m = max_of<T>(v[j], m);
+        stay_packed<T>(v);
+        under(q, m);
+#pragma unroll
+        for (int j = 0; j < U; ++j) add_unit<T>(v[j], m, q.s, q.t);
+    }
+    under(q, row_max(lds, q.m, waves));
+    row_sums(lds, q, waves);
+    return q;
+}
+
 // Rows that no workgroup's registers hold, and the gradient from stored statistics, which needs nothing held: the row is read for either part.
 template <class T, bool STATS, bool GRAD>
 __global__ void __launch_bounds__(1024) policy_stream_kernel(PolicyArgs a)
@@ -312,26 +340,14 @@ __global__ void __launch_bounds__(1024) policy_stream_kernel(PolicyArgs a)
     constexpr int V = Unit<T>::V;
     __shared__ RowLds lds;
     const int64_t n = blockIdx.x;
-    const int tid = threadIdx.x, threads = blockDim.x, waves = threads >> 6, K = a.K, stride = threads * V;
+    const int tid = threadIdx.x, threads = blockDim.x, K = a.K, stride = threads * V;
     const Row r = load_row(a, n);
     const T *x = static_cast<const T *>(a.logits) + n * a.pitch;
     const float xa = logit_of_action(x, r, K);
     Slope g;
     if constexpr (STATS) {
         Sums q = {LOWEST, 0.f, 0.f};
-        if (!r.idle) {                       // (uniform)
-            for (int k0 = tid * V; k0 < K; k0 += stride) {
-                const typename Unit<T>::raw v = load_unit<T>(x, k0, K);
-                const float m = max_of<T>(v, q.m), d = fmaxf((q.m - m) * LOG2E, FAR), scale = __builtin_amdgcn_exp2f(d);
-                q.t = scale * fmaf(q.s, d, q.t);
-                q.s *= scale;
-                q.m = m;
-                add_unit<T>(v, m, q.s, q.t);
-            }
-            const float m = row_max(lds, q.m, waves), d = fmaxf((q.m - m) * LOG2E, FAR), scale = __builtin_amdgcn_exp2f(d);
-            q = {m, q.s * scale, scale * fmaf(q.s, d, q.t)};
-            row_sums(lds, q, waves);
-        }
+        if (!r.idle) q = running_sums<T>(lds, x, 0, (K + V - 1) / V, K);         // (uniform)
         float loss;
         g = finish_row(a, n, r, q, xa, tid == 0, loss);
         if (tid == 0) a.part_loss[n] = loss;
@@ -347,6 +363,97 @@ __global__ void __launch_bounds__(1024) policy_stream_kernel(PolicyArgs a)
             for (int i = 0; i < V; ++i) v[i] = (T)0.f;
             if (!g.idle) v = load_unit<T>(x, k0, K);
             store_unit<T>(dx, k0, K, gradient<T>(v, k0, g));
+        }
+    }
+}
+
+// Few long rows: a row in pieces, a workgroup each, joined in the launch behind.  Partial sums lie as [N][pieces] m, s, t; then [N] the logits of the actions, which
+// another piece's gradient may be stored over.
+struct Pieces { int units, count; float *sums, *xa; };
+constexpr int MAX_PIECES = 64;
+template <class T>
+__global__ void __launch_bounds__(256) policy_piece_kernel(PolicyArgs a, Pieces c)
+{
+    constexpr int V = Unit<T>::V;
+    __shared__ RowLds lds;
+    const int64_t n = blockIdx.x / (unsigned)c.count;
+    const int piece = (int)(blockIdx.x - n * c.count), units = (a.K + V - 1) / V;
+    const Row r = load_row(a, n);
+    if (r.idle) return;                      // (uniform)
+    const T *x = static_cast<const T *>(a.logits) + n * a.pitch;
+    const Sums q = running_sums<T>(lds, x, piece * c.units, min((piece + 1) * c.units, units), a.K);
+    if (threadIdx.x == 0) {
+        float *o = c.sums + 3 * (n * c.count + piece);
+        o[0] = q.m; o[1] = q.s; o[2] = q.t;
+        if (piece == 0) c.xa[n] = logit_of_action(x, r, a.K);
+    }
+}
+__device__ __forceinline__ Sums joined(const Pieces &c, int64_t n)
+{
+    const float *p = c.sums + 3 * n * c.count;
+    float m = LOWEST;
+    for (int i = 0; i < c.count; ++i) m = fmaxf(m, p[3 * i]);
+    Sums q = {m, 0.f, 0.f};
+    for (int i = 0; i < c.count; ++i) {
+        const float d = fmaxf((p[3 * i] - m) * LOG2E, FAR), scale = __builtin_amdgcn_exp2f(d), s = p[3 * i + 1];
+        q.s += s * scale;
+        q.t += scale * fmaf(s, d, p[3 * i + 2]);
+    }
+    return q;
+}
+// the rows' results, a thread each, and the loss
+__global__ void __launch_bounds__(256) policy_join_kernel(PolicyArgs a, Pieces c, float *__restrict__ loss_out)
+{
+    __shared__ double red[4];
+    const int n = threadIdx.x;
+    float loss = 0.f;
+    if (n < a.N) {
+        const Row r = load_row(a, n);
+        const Sums q = r.idle ? Sums{LOWEST, 0.f, 0.f} : joined(c, n);
+        finish_row(a, n, r, q, r.idle ? 0.f : c.xa[n], true, loss);
+    }
+    double s = loss;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
+    if ((n & 63) == 0) red[n >> 6] = s;
+    __syncthreads();
+    if (n == 0) {
+        for (int k = 1; k < (int)blockDim.x >> 6; ++k) s += red[k];
+        loss_out[0] = (float)s;
+    }
+}
+// a piece's gradient; every workgroup of a row joins its pieces for itself, or takes what a forward pass stored (not over the logits: one workgroup would read the
+// action's logit where another had stored the gradient)
+template <class T, bool STORED>
+__global__ void __launch_bounds__(256) policy_piece_gradient_kernel(PolicyArgs a, Pieces c)
+{
+    constexpr int V = Unit<T>::V;
+    const int64_t n = blockIdx.x / (unsigned)c.count;
+    const int piece = (int)(blockIdx.x - n * c.count), units = (a.K + V - 1) / V, last = min((piece + 1) * c.units, units);
+    const Row r = load_row(a, n);
+    const T *x = static_cast<const T *>(a.logits) + n * a.pitch;
+    T *dx = static_cast<T *>(a.dlogits) + n * a.dpitch;
+    Slope g;
+    if constexpr (STORED) {
+        g = stored_row(a, n, r, logit_of_action(x, r, a.K));
+    } else {
+        const bool first = piece == 0 && threadIdx.x == 0;
+        float loss;
+        g = finish_row(a, n, r, r.idle ? Sums{LOWEST, 0.f, 0.f} : joined(c, n), r.idle ? 0.f : c.xa[n], first, loss);
+        if (first) a.part_loss[n] = loss;
+    }
+    for (int u = piece * c.units + (int)threadIdx.x; u < last; u += 4 * 256) {
+        typename Unit<T>::raw v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[j][i] = (T)0.f;
+            if (!g.idle && u + j * 256 < last) v[j] = load_unit<T>(x, (u + j * 256) * V, a.K);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int k0 = (u + j * 256) * V;
+            if (u + j * 256 < last) store_unit<T>(dx, k0, a.K, gradient<T>(v[j], k0, g));
         }
     }
 }
@@ -395,6 +502,16 @@ ssm_status check_gradient(const PolicyArgs &a, int dtype, int64_t N, int64_t K)
     return N > 1 && a.dpitch > SSM_MAX_ELEMS / N ? SSM_ERR_UNSUPPORTED : SSM_OK;
 }
 
+// Few long rows go in pieces: a workgroup works through 65536 logits in about 6 us, whatever the other CUs do.  us, a workgroup per row and in pieces (forward; loss
+// and gradient), bf16:  1 x 65536: 10.0, 7.2; 15.8, 9.9    16 x 65536: 10.4, 7.5; 16.3, 10.3    64 x 65536: 10.5, 8.3; 17.1, 12.5    4 x 300000: 28.7, 13.3; 52.6, 14.4
+// and not:  16 x 16384: 6.3, 6.9; 8.2, 9.7    64 x 16384: 6.4, 6.6; 8.4, 9.8    128 x 32768: 8.2, 7.7; 12.1, 12.7    256 x 65536: 11.9, 13.7; 23.1, 26.4
+constexpr int64_t PIECES_MAX_ROWS = 64, PIECES_MIN_UNITS = 4096, PIECE_UNITS = 256 * 4;
+int pieces_of(int64_t N, int64_t units)
+{
+    if (N > PIECES_MAX_ROWS || units <= PIECES_MIN_UNITS) return 0;
+    return units <= PIECE_UNITS * MAX_PIECES ? (int)((units + PIECE_UNITS - 1) / PIECE_UNITS) : MAX_PIECES;
+}
+
 // Who holds a row: part of a wavefront, a wavefront, a workgroup, or nobody.
 // Returns the number of parts of the loss.
 template <class T, bool STATS, bool GRAD> int64_t launch_rows_of(const PolicyArgs &a, hipStream_t s)
@@ -431,6 +548,21 @@ template <class T, bool STATS, bool GRAD> int64_t launch_rows_of(const PolicyArg
 }
 template <bool STATS, bool GRAD> ssm_status launch_rows(const PolicyArgs &a, int dtype, float *loss, hipStream_t s)
 {
+    const int64_t units = ((int64_t)a.K * (int64_t)dtype_bytes(dtype) + 15) / 16;
+    const int count = pieces_of(a.N, units);
+    if (count && (STATS || a.dlogits != a.logits)) {
+        Pieces c{(int)((units + count - 1) / count), count, STATS ? a.part_loss + PIECES_MAX_ROWS : nullptr, nullptr};
+        if (STATS) c.xa = c.sums + 3 * a.N * count;
+        const dim3 grid((unsigned)(a.N * count));
+        with_dtype(dtype, [&](auto t) {
+            using T = decltype(t);
+            if constexpr (STATS) hipLaunchKernelGGL(policy_piece_kernel<T>, grid, dim3(256), 0, s, a, c);
+            if constexpr (GRAD) hipLaunchKernelGGL((policy_piece_gradient_kernel<T, !STATS>), grid, dim3(256), 0, s, a, c);
+        });
+        if constexpr (STATS && GRAD) hipLaunchKernelGGL(policy_sum_kernel, dim3(1), dim3(64), 0, s, a.part_loss, a.N, loss);
+        else if constexpr (STATS) hipLaunchKernelGGL(policy_join_kernel, dim3(1), dim3(64), 0, s, a, c, loss);
+        return hipGetLastError() == hipSuccess ? SSM_OK : SSM_ERR_HIP;
+    }
     const int64_t parts = with_dtype(dtype, [&](auto t) { return launch_rows_of<decltype(t), STATS, GRAD>(a, s); });
     if (hipGetLastError() != hipSuccess) return SSM_ERR_HIP;
     if constexpr (STATS) {
@@ -450,7 +582,9 @@ extern "C" {
 size_t ssm_policy_loss_workspace_bytes(int64_t N, int64_t K)
 {
     if (N <= 0 || K <= 0 || N > SSM_MAX_TOKENS || K > (1LL << 30) || K > SSM_MAX_ELEMS / N) return 0;
-    return ((size_t)(N + 3) * 4 + ALIGN - 1) / ALIGN * ALIGN;      // (four wavefronts' parts from one row on)
+    // parts of the loss (four wavefronts' from one row on); few rows, which may go in pieces: the pieces' sums and the actions' logits
+    const size_t floats = N <= PIECES_MAX_ROWS ? PIECES_MAX_ROWS + (3 * MAX_PIECES + 1) * (size_t)N : (size_t)N + 3;
+    return (floats * 4 + ALIGN - 1) / ALIGN * ALIGN;
 }
 
 ssm_status ssm_policy_loss_fwd(const void *logits, int64_t pitch, const int64_t *action, const float *logp_old,

@@ -62,7 +62,8 @@ def _compare(s, dtype, terms=TERMS):
 
 
 SHAPES = [(1, 1), (3, 2), (5, 3), (64, 7), (33, 32), (17, 33), (9, 64), (300, 65), (4, 255), (6, 256), (2, 1000), (3, 1025), (2, 2048), (7, 5003),
-          (1, 16384), (2, 20001), (1, 40000), (2, 70001), (1, 140000), (1, 300001)]
+          (1, 16384), (2, 20001), (1, 40000), (2, 70001), (1, 140000), (1, 300001),
+          (64, 9001), (65, 9001), (40, 16400), (2, 1200003)]
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
