@@ -43,8 +43,9 @@ __device__ __forceinline__ float wave_max(float v)
     return v;
 }
 
-// What is given per row, and what comes of it.  The few numbers of a row are computed in 64 bits: in 32 the logarithm of a large sum alone would put
-// a ratio off by 5e-7.
+// What is given per row, and what comes of it.  Sums and differences of a row's few numbers are formed in 64 bits (in 32, the logarithm of a large sum alone would put a
+// ratio off by 5e-7), functions of them in 32 where their argument is small or its rounded part is put back.  (With the 64-bit functions a row cost its wavefront
+// some 2500 cycles, more than the logits of a short one: 65536 x 200 bf16 forward 28.6 us, with these ROWTERMS.)
 struct Row {
     int64_t action;
     float old, advantage, ref, weight;
@@ -60,20 +61,37 @@ __device__ __forceinline__ Row load_row(const PolicyArgs &a, int64_t n)
     r.idle = r.weight == 0.f || r.action < 0;
     return r;
 }
-struct Terms { double loss, slope; };        // of the row's loss, and of it with respect to logp
-__device__ __forceinline__ Terms row_terms(const PolicyArgs &a, const Row &r, double logp, double entropy)
+struct Terms { float loss, slope; };         // of the row's loss, and of it with respect to logp
+__device__ __forceinline__ Terms row_terms(const PolicyArgs &a, const Row &r, double logp, float entropy)
 {
-    const double A = r.advantage, rho = exp(logp - (double)r.old), low = 1.0 - (double)a.terms.clip_low, high = 1.0 + (double)a.terms.clip_high;
+    const double gap = logp - (double)r.old;
+    const float g = (float)gap, A = r.advantage, rho0 = expf(g), rho = fmaf(rho0, (float)(gap - (double)g), rho0);
+    const float low = 1.f - a.terms.clip_low, high = 1.f + a.terms.clip_high;
     // (an advantage of zero makes the term zero, also where the ratio overflows)
-    const double raw = A == 0.0 ? 0.0 : rho * A, clipped = (rho < low ? low : rho > high ? high : rho) * A;
+    const float ratio = rho0 == INFINITY ? rho0 : rho;
+    const float raw = A == 0.f ? 0.f : ratio * A, clipped = (ratio < low ? low : ratio > high ? high : ratio) * A;
     const bool held = clipped < raw;         // (a NaN is not held: it reaches the results)
-    Terms t = {-(held ? clipped : raw) - (double)a.terms.entropy_coef * entropy, held ? 0.0 : -raw};
+    Terms t = {-(held ? clipped : raw) - a.terms.entropy_coef * entropy, held ? 0.f : -raw};
     if (a.logp_ref) {
-        const double d = (double)r.ref - logp, e = expm1(d);
-        t.loss += (double)a.terms.kl_coef * (e - d);
-        t.slope -= (double)a.terms.kl_coef * e;
+        // e^d - 1 - d cancels to d^2 / 2: its series up to a half, whose first term left out is 1e-9 of it
+        const float d = (float)((double)r.ref - logp);
+        float p = 1.f / 3628800.f;
+        p = fmaf(p, d, 1.f / 362880.f); p = fmaf(p, d, 1.f / 40320.f); p = fmaf(p, d, 1.f / 5040.f); p = fmaf(p, d, 1.f / 720.f);
+        p = fmaf(p, d, 1.f / 120.f); p = fmaf(p, d, 1.f / 24.f); p = fmaf(p, d, 1.f / 6.f); p = fmaf(p, d, 0.5f);
+        const bool near = fabsf(d) < 0.5f;
+        const float far = expf(d) - 1.f, k = near ? p * d * d : far - d, e = near ? d + k : far;
+        t.loss += a.terms.kl_coef * k;
+        t.slope -= a.terms.kl_coef * e;
     }
     return t;
+}
+// log s for s > 0: the exponent's part in 64 bits, the rest between log 0.75 and log 1.5
+__device__ __forceinline__ double log_of_sum(float s)
+{
+    int e;
+    float f = frexpf(s, &e);                 // [0.5, 1)
+    if (f < 0.75f) { f *= 2.f; --e; }
+    return (double)e * 0.6931471805599453 + (double)logf(f);
 }
 
 // Sums of a row (of a part of one): largest logit m, s = sum 2^d, t = sum 2^d d with d = (x - m) log2 e.  m starts at the lowest number, not at -infinity: a row with
@@ -164,25 +182,26 @@ template <class T> __device__ __forceinline__ typename Unit<T>::wide gradient(ty
 __device__ __forceinline__ Slope finish_row(const PolicyArgs &a, int64_t n, const Row &r, const Sums &q, float xa, bool store, float &loss)
 {
     const bool idle = r.idle || q.s == 0.f;
-    const double ls = log((double)q.s), entropy = ls - (double)q.t * 0.6931471805599453 / (double)q.s, logp = ((double)xa - (double)q.m) - ls;
+    const double ls = log_of_sum(q.s), logp = ((double)xa - (double)q.m) - ls;
+    const float entropy = (float)(ls - (double)(q.t * 0.69314718f / q.s));
     const Terms t = row_terms(a, r, logp, entropy);
-    loss = idle ? 0.f : (float)((double)r.weight * t.loss);
+    loss = idle ? 0.f : r.weight * t.loss;
     if (store) {
         a.logp[n] = idle ? 0.f : (float)logp;
-        a.entropy[n] = idle ? 0.f : (float)entropy;
+        a.entropy[n] = idle ? 0.f : entropy;
         a.lse[n] = idle ? -INFINITY : (float)((double)q.m + ls);
     }
-    const double w = (double)r.weight * (a.dloss ? (double)a.dloss[0] : 1.0), eta = w * (double)a.terms.entropy_coef, slope = w * t.slope;
-    return {q.m, (float)(-ls * 1.4426950408889634), (float)(eta * entropy - slope), (float)(eta * 0.6931471805599453), (float)slope, (int)r.action, idle};
+    const float w = r.weight * (a.dloss ? a.dloss[0] : 1.f), eta = w * a.terms.entropy_coef, slope = w * t.slope;
+    return {q.m, (float)(-ls * 1.4426950408889634), fmaf(eta, entropy, -slope), eta * 0.69314718f, slope, (int)r.action, idle};
 }
 // The same from what the forward pass stored.  (Differences from the logit of the action, not from lse: lse is rounded by 10^-3 at logits of 10^4.)
 __device__ __forceinline__ Slope stored_row(const PolicyArgs &a, int64_t n, const Row &r, float xa)
 {
     const float lse = a.lse[n], logp = a.logp[n], entropy = a.entropy[n];
     const Terms t = row_terms(a, r, logp, entropy);
-    const double w = (double)r.weight * (a.dloss ? (double)a.dloss[0] : 1.0), eta = w * (double)a.terms.entropy_coef, slope = w * t.slope;
+    const float w = r.weight * (a.dloss ? a.dloss[0] : 1.f), eta = w * a.terms.entropy_coef, slope = w * t.slope;
     const bool taken = xa != -INFINITY;      // (else the action cannot be taken and its logit is no reference)
-    return {taken ? xa : lse, taken ? logp * LOG2E : 0.f, (float)(eta * (double)entropy - slope), (float)(eta * 0.6931471805599453), (float)slope, (int)r.action,
+    return {taken ? xa : lse, taken ? logp * LOG2E : 0.f, fmaf(eta, entropy, -slope), eta * 0.69314718f, slope, (int)r.action,
             r.idle || lse == -INFINITY};
 }
 template <class T> __device__ __forceinline__ float logit_of_action(const T *x, const Row &r, int K)
