@@ -30,22 +30,39 @@ struct PolicyArgs {
     float mean_weight;                       // of a row where none are given
 };
 
-__device__ __forceinline__ float wave_sum(float v)
+// Over groups of 2^lanes neighbouring lanes, the result in all of them, without a trip through LDS: lanes exchange within four, within eight and sixteen by mirroring
+// (their fours and eights hold one value by then), rows of sixteen and halves of the wavefront by swaps.
+template <int CONTROL> __device__ __forceinline__ float exchanged(float v)
 {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    const int x = __builtin_bit_cast(int, v);
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(x, x, CONTROL, 0xf, 0xf, false));
+}
+template <class F> __device__ __forceinline__ float over_group(float v, int lanes, F op)
+{
+    if (lanes >= 1) v = op(v, exchanged<0xb1>(v));           // quad_perm 1 0 3 2
+    if (lanes >= 2) v = op(v, exchanged<0x4e>(v));           // quad_perm 2 3 0 1
+    if (lanes >= 3) v = op(v, exchanged<0x141>(v));          // row_half_mirror
+    if (lanes >= 4) v = op(v, exchanged<0x140>(v));          // row_mirror
+    if (lanes >= 5) {
+        const unsigned x = __float_as_uint(v);
+        const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+        v = op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+    if (lanes >= 6) {
+        const unsigned x = __float_as_uint(v);
+        const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+        v = op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
     return v;
 }
-__device__ __forceinline__ float wave_max(float v)
-{
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
-    return v;
-}
+__device__ __forceinline__ float group_sum(float v, int lanes) { return over_group(v, lanes, [](float a, float b) { return a + b; }); }
+__device__ __forceinline__ float group_max(float v, int lanes) { return over_group(v, lanes, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ __forceinline__ float wave_sum(float v) { return group_sum(v, 6); }
+__device__ __forceinline__ float wave_max(float v) { return group_max(v, 6); }
 
 // What is given per row, and what comes of it.  Sums and differences of a row's few numbers are formed in 64 bits (in 32, the logarithm of a large sum alone would put a
 // ratio off by 5e-7), functions of them in 32 where their argument is small or its rounded part is put back.  (With the 64-bit functions a row cost its wavefront
-// some 2500 cycles, more than the logits of a short one: 65536 x 200 bf16 forward 28.6 us, with these ROWTERMS.)
+// some 2500 cycles, more than the logits of a short one: 65536 x 200 bf16 forward 28.6 us, with these 22.5.)
 struct Row {
     int64_t action;
     float old, advantage, ref, weight;
@@ -104,15 +121,29 @@ template <class T> struct Unit {             // 16 bytes of a row
     typedef typename Pack<T, V>::type raw;
     typedef float wide __attribute__((ext_vector_type(V)));
 };
-// unit from element k0 on; what lies past the end of the row is an action that cannot be taken
+// unit from element k0 on; what lies past the end of the row is an action that cannot be taken.  (As words on both sides: put together element by element, the compiler gives
+// a 16-bit element a register of its own, four units more than 100 of them.)
 template <class T> __device__ __forceinline__ typename Unit<T>::raw load_unit(const T *x, int k0, int K)
 {
+    typedef unsigned words __attribute__((ext_vector_type(4)));
+    typedef typename std::conditional<sizeof(T) == 2, uint16_t, uint32_t>::type bits;
     constexpr int V = Unit<T>::V;
-    if (K - k0 >= V) return load_pack<T, V>(x + k0);
-    typename Unit<T>::raw v;
+    words w;
+    if (K - k0 >= V) {
+        w = __builtin_bit_cast(words, load_pack<T, V>(x + k0));
+    } else {
+        const unsigned none = __builtin_bit_cast(bits, (T)-INFINITY);
+        const bits *q = reinterpret_cast<const bits *>(x);
+        unsigned e[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = k0 + i < K ? x[k0 + i] : (T)-INFINITY;
-    return v;
+        for (int i = 0; i < V; ++i) e[i] = k0 + i < K ? (unsigned)q[k0 + i] : none;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (V == 8) w[i] = e[2 * i] | e[2 * i + 1] << 16;
+            else w[i] = e[i];
+        }
+    }
+    return __builtin_bit_cast(typename Unit<T>::raw, w);
 }
 template <class T> __device__ __forceinline__ void store_unit(T *x, int k0, int K, typename Unit<T>::wide g)
 {
@@ -124,15 +155,16 @@ template <class T> __device__ __forceinline__ void store_unit(T *x, int k0, int 
 }
 template <class T> __device__ __forceinline__ typename Unit<T>::wide widen(typename Unit<T>::raw v) { return __builtin_convertvector(v, typename Unit<T>::wide); }
 
-// (16-bit units stay packed from one sweep over them to the next: widened ones would not fit the registers)
-template <class T, int U> __device__ __forceinline__ void stay_packed(typename Unit<T>::raw (&v)[U])
+// (16-bit units stay packed from one sweep over them to the next, and until `known` is: widened ones, or such that are widened ahead of what they wait for, would not
+// fit the registers)
+template <class T, int U> __device__ __forceinline__ void stay_packed(typename Unit<T>::raw (&v)[U], float &known)
 {
     typedef unsigned words __attribute__((ext_vector_type(4)));
     if constexpr (sizeof(T) == 2) {
 #pragma unroll
         for (int j = 0; j < U; ++j) {
             words w = __builtin_bit_cast(words, v[j]);
-            asm volatile("" : "+v"(w));
+            asm volatile("" : "+v"(w), "+v"(known));
             v[j] = __builtin_bit_cast(typename Unit<T>::raw, w);
         }
     }
@@ -209,51 +241,52 @@ template <class T> __device__ __forceinline__ float logit_of_action(const T *x, 
     return r.idle ? 0.f : r.action < K ? (float)x[r.action] : NAN;
 }
 
-// Short rows: 2^lanes neighbouring lanes hold a row, U units of 16 bytes each (U > 1: the whole wavefront), so a wavefront holds 64 >> lanes of them.
-template <class T, int U, bool STATS, bool GRAD>
+// Short rows: 2^lanes neighbouring lanes hold a row, one unit of 16 bytes each, so a wavefront holds R = 64 >> lanes of them at a time and B such batches. What is
+// computed once per row would cost as much as its logits do; lane j does it for row j of the R B <= 64.  (65536 x 200 bf16, one batch and eight (forward) or four: forward
+// 20.9 -> 16.4 us, loss and gradient 28.0 -> 23.6; 65536 x 512: 34.4 -> 26.2, 47.5 -> 38.0.)
+template <class T, int B, bool STATS, bool GRAD>
 __global__ void __launch_bounds__(256) policy_wave_kernel(PolicyArgs a, int lanes)
 {
     constexpr int V = Unit<T>::V;
-    const int lane = threadIdx.x & 63, width = 1 << lanes, sub = lane & (width - 1), K = a.K;
-    const int64_t want = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * (64 >> lanes) + (lane >> lanes), n = want < a.N ? want : a.N - 1;
-    const Row r = load_row(a, n);
-    const T *x = static_cast<const T *>(a.logits) + n * a.pitch;
-    const float xa = logit_of_action(x, r, K);
-    typename Unit<T>::raw v[U];
+    const int lane = threadIdx.x & 63, width = 1 << lanes, k0 = (lane & (width - 1)) * V, group = lane >> lanes, R = 64 >> lanes, K = a.K;
+    const int64_t first = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * (R * B);
+    const auto row_of = [&](int j) { const int64_t n = first + j; return n < a.N ? n : a.N - 1; };
+    typename Unit<T>::raw v[B];
 #pragma unroll
-    for (int j = 0; j < U; ++j) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) v[j][i] = (T)-INFINITY;
+    for (int b = 0; b < B; ++b) v[b] = load_unit<T>(static_cast<const T *>(a.logits) + row_of(b * R + group) * a.pitch, k0, K);
+    const int64_t mine = row_of(lane);
+    const bool own = lane < R * B && first + lane < a.N;
+    Row r{-1, 0.f, 0.f, 0.f, 0.f, true};
+    float xa = 0.f;
+    if (own) {
+        r = load_row(a, mine);
+        xa = logit_of_action(static_cast<const T *>(a.logits) + mine * a.pitch, r, K);
     }
-    if (!r.idle) {
-#pragma unroll
-        for (int j = 0; j < U; ++j) v[j] = load_unit<T>(x, (sub + j * width) * V, K);
-    }
-    Slope g;
+    Slope g{};
     if constexpr (STATS) {
         Sums q = {LOWEST, 0.f, 0.f};
+        const int from = (lane & (R - 1)) << lanes, batch = lane >> (6 - lanes);     // who holds row `lane`: that group, of that batch
 #pragma unroll
-        for (int j = 0; j < U; ++j) q.m = max_of<T>(v[j], q.m);
-        for (int o = 1; o < width; o <<= 1) q.m = fmaxf(q.m, __shfl_xor(q.m, o));
-        stay_packed<T>(v);
-#pragma unroll
-        for (int j = 0; j < U; ++j) add_unit<T>(v[j], q.m, q.s, q.t);
-        for (int o = 1; o < width; o <<= 1) { q.s += __shfl_xor(q.s, o); q.t += __shfl_xor(q.t, o); }
-        stay_packed<T>(v);
-        const bool mine = sub == 0 && want < a.N;
+        for (int b = 0; b < B; ++b) {
+            Sums p = {group_max(max_of<T>(v[b], LOWEST), lanes), 0.f, 0.f};
+            add_unit<T>(v[b], p.m, p.s, p.t);
+            p = {__shfl(p.m, from), __shfl(group_sum(p.s, lanes), from), __shfl(group_sum(p.t, lanes), from)};
+            q = {batch == b ? p.m : q.m, batch == b ? p.s : q.s, batch == b ? p.t : q.t};
+        }
         float loss;
-        g = finish_row(a, n, r, q, xa, mine, loss);
-        loss = wave_sum(mine ? loss : 0.f);
+        g = finish_row(a, mine, r, q, xa, own, loss);
+        loss = wave_sum(own ? loss : 0.f);
         if (lane == 0) a.part_loss[(int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)] = loss;
-    } else {
-        g = stored_row(a, n, r, xa);
+    } else if (own) {
+        g = stored_row(a, mine, r, xa);
     }
     if constexpr (GRAD) {
-        T *dx = static_cast<T *>(a.dlogits) + n * a.dpitch;
+        if (g.idle) g.action = -2;
 #pragma unroll
-        for (int j = 0; j < U; ++j) {
-            const int k0 = (sub + j * width) * V;
-            if (want < a.N && k0 < K) store_unit<T>(dx, k0, K, gradient<T>(v[j], k0, g));
+        for (int b = 0; b < B; ++b) {
+            const int j = b * R + group, action = __shfl(g.action, j);
+            const Slope h = {__shfl(g.base, j), __shfl(g.off, j), __shfl(g.c, j), __shfl(g.eta, j), __shfl(g.slope, j), action, action == -2};
+            if (first + j < a.N && k0 < K) store_unit<T>(static_cast<T *>(a.dlogits) + row_of(j) * a.dpitch, k0, K, gradient<T>(v[b], k0, h));
         }
     }
 }
@@ -278,7 +311,7 @@ __device__ __forceinline__ void row_sums(RowLds &lds, Sums &q, int waves)
     for (int w = 1; w < waves; ++w) { q.s += lds.s[w]; q.t += lds.t[w]; }
 }
 
-// Longer rows: a workgroup holds one in registers, U units of 16 bytes per thread, and reads it once.
+// Longer rows: a workgroup (of one wavefront up to sixteen) holds one in registers, U units of 16 bytes per thread, and reads it once.
 template <class T, int U, bool GRAD>
 __global__ void __launch_bounds__(1024) policy_row_kernel(PolicyArgs a)
 {
@@ -307,10 +340,10 @@ __global__ void __launch_bounds__(1024) policy_row_kernel(PolicyArgs a)
 #pragma unroll
         for (int j = 0; j < U; ++j) q.m = max_of<T>(v[j], q.m);
         q.m = row_max(lds, q.m, waves);
-        stay_packed<T>(v);
+        stay_packed<T>(v, q.m);
 #pragma unroll
         for (int j = 0; j < U; ++j) add_unit<T>(v[j], q.m, q.s, q.t);
-        stay_packed<T>(v);
+        stay_packed<T>(v, q.s);
         row_sums(lds, q, waves);             // (behind its barrier the gradient may be stored over the logits)
         g = finish_row(a, n, r, q, xa, tid == 0, loss);
     }
@@ -342,7 +375,7 @@ template <class T> __device__ __forceinline__ Sums running_sums(RowLds &lds, con
         for (int j = 0; j < U; ++j) v[j] = load_unit<T>(x, u + j * threads < last ? (u + j * threads) * V : K, K);
 #pragma unroll
         for (int j = 0; j < U; ++j) m = max_of<T>(v[j], m);
-        stay_packed<T>(v);
+        stay_packed<T>(v, m);
         under(q, m);
 #pragma unroll
         for (int j = 0; j < U; ++j) add_unit<T>(v[j], m, q.s, q.t);
@@ -537,32 +570,37 @@ template <class T, bool STATS, bool GRAD> int64_t launch_rows_of(const PolicyArg
 {
     constexpr int V = Unit<T>::V;
     const int64_t units = ((int64_t)a.K + V - 1) / V;
-    const auto wave = [&](auto u, int lanes) {
-        const int64_t rows = 4 * (64 >> lanes);
-        const int64_t blocks = (a.N + rows - 1) / rows;
-        hipLaunchKernelGGL((policy_wave_kernel<T, decltype(u)::value, STATS, GRAD>), dim3((unsigned)blocks), dim3(256), 0, s, a, lanes);
-        return 4 * blocks;
-    };
     if (units <= 64) {
         int lanes = 0;
         while ((1 << lanes) < units) ++lanes;
-        return wave(std::integral_constant<int, 1>{}, lanes);
+        const auto wave = [&](auto batches) {
+            constexpr int B = decltype(batches)::value;
+            const int64_t rows = 4 * (64 >> lanes) * B, blocks = (a.N + rows - 1) / rows;
+            hipLaunchKernelGGL((policy_wave_kernel<T, B, STATS, GRAD>), dim3((unsigned)blocks), dim3(256), 0, s, a, lanes);
+            return 4 * blocks;
+        };
+        // (as many batches as leave two wavefronts to a SIMD; eight with a gradient would take half the wavefronts of a SIMD for their registers)
+        const int64_t waves = a.N >> (6 - lanes);
+        if constexpr (!GRAD) { if (lanes >= 3 && waves >= 8 * 2048) return wave(std::integral_constant<int, 8>{}); }
+        if (lanes >= 2 && waves >= 4 * 2048) return wave(std::integral_constant<int, 4>{});
+        if (lanes >= 1 && waves >= 2 * 2048) return wave(std::integral_constant<int, 2>{});
+        return wave(std::integral_constant<int, 1>{});
     }
-    if (units <= 128) return wave(std::integral_constant<int, 2>{}, 6);
-    if (units <= 256) return wave(std::integral_constant<int, 4>{}, 6);
-    if (units <= 512) return wave(std::integral_constant<int, 8>{}, 6);
     if constexpr (STATS) {
         const auto row = [&](auto u, int threads) {
             hipLaunchKernelGGL((policy_row_kernel<T, decltype(u)::value, GRAD>), dim3((unsigned)a.N), dim3(threads), 0, s, a);
             return a.N;
         };
+        if (units <= 64 * 2) return row(std::integral_constant<int, 2>{}, 64);
+        if (units <= 64 * 4) return row(std::integral_constant<int, 4>{}, 64);
+        if (units <= 64 * 8) return row(std::integral_constant<int, 8>{}, 64);
         if (units <= 256 * 4) return row(std::integral_constant<int, 4>{}, 256);
         if (units <= 256 * 8) return row(std::integral_constant<int, 8>{}, 256);
         if (units <= 512 * 8) return row(std::integral_constant<int, 8>{}, 512);
         if (units <= 512 * 16) return row(std::integral_constant<int, 16>{}, 512);
         if (units <= 1024 * 16) return row(std::integral_constant<int, 16>{}, 1024);
     }
-    hipLaunchKernelGGL((policy_stream_kernel<T, STATS, GRAD>), dim3((unsigned)a.N), dim3(units <= 2048 ? 256 : 1024), 0, s, a);
+    hipLaunchKernelGGL((policy_stream_kernel<T, STATS, GRAD>), dim3((unsigned)a.N), dim3(units <= 256 ? 64 : units <= 2048 ? 256 : 1024), 0, s, a);
     return a.N;
 }
 template <bool STATS, bool GRAD> ssm_status launch_rows(const PolicyArgs &a, int dtype, float *loss, hipStream_t s)
