@@ -26,7 +26,7 @@ struct PolicyArgs {
     float *logp, *entropy, *lse;             // written by the forward pass, read by the gradient pass on its own
     const float *dloss;
     void *dlogits; int64_t dpitch;
-    float *part_loss;                        // weighted, of every workgroup's row or every wavefront's rows
+    float *part_loss;                        // weighted, of every workgroup's rows
     float mean_weight;                       // of a row where none are given
 };
 
@@ -248,6 +248,7 @@ template <class T, int B, bool STATS, bool GRAD>
 __global__ void __launch_bounds__(256) policy_wave_kernel(PolicyArgs a, int lanes)
 {
     constexpr int V = Unit<T>::V;
+    __shared__ float red[4];
     const int lane = threadIdx.x & 63, width = 1 << lanes, k0 = (lane & (width - 1)) * V, group = lane >> lanes, R = 64 >> lanes, K = a.K;
     const int64_t first = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * (R * B);
     const auto row_of = [&](int j) { const int64_t n = first + j; return n < a.N ? n : a.N - 1; };
@@ -276,7 +277,9 @@ __global__ void __launch_bounds__(256) policy_wave_kernel(PolicyArgs a, int lane
         float loss;
         g = finish_row(a, mine, r, q, xa, own, loss);
         loss = wave_sum(own ? loss : 0.f);
-        if (lane == 0) a.part_loss[(int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)] = loss;
+        if (lane == 0) red[threadIdx.x >> 6] = loss;
+        __syncthreads();
+        if (threadIdx.x == 0) a.part_loss[blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
     } else if (own) {
         g = stored_row(a, mine, r, xa);
     }
@@ -565,8 +568,8 @@ int pieces_of(int64_t N, int64_t units)
 }
 
 // Who holds a row: part of a wavefront, a wavefront, a workgroup, or nobody.
-// Returns the number of parts of the loss.
-template <class T, bool STATS, bool GRAD> int64_t launch_rows_of(const PolicyArgs &a, hipStream_t s)
+// Workgroups, and so parts of the loss.  With one, its part is the loss: `a.part_loss` is where that goes then (set here), and nothing is left to add up.
+template <class T, bool STATS, bool GRAD> int64_t launch_rows_of(PolicyArgs &a, float *loss, hipStream_t s)
 {
     constexpr int V = Unit<T>::V;
     const int64_t units = ((int64_t)a.K + V - 1) / V;
@@ -576,8 +579,9 @@ template <class T, bool STATS, bool GRAD> int64_t launch_rows_of(const PolicyArg
         const auto wave = [&](auto batches) {
             constexpr int B = decltype(batches)::value;
             const int64_t rows = 4 * (64 >> lanes) * B, blocks = (a.N + rows - 1) / rows;
+            if (blocks == 1) a.part_loss = loss;
             hipLaunchKernelGGL((policy_wave_kernel<T, B, STATS, GRAD>), dim3((unsigned)blocks), dim3(256), 0, s, a, lanes);
-            return 4 * blocks;
+            return blocks;
         };
         // (as many batches as leave two wavefronts to a SIMD; eight with a gradient would take half the wavefronts of a SIMD for their registers)
         const int64_t waves = a.N >> (6 - lanes);
@@ -586,6 +590,7 @@ template <class T, bool STATS, bool GRAD> int64_t launch_rows_of(const PolicyArg
         if (lanes >= 1 && waves >= 2 * 2048) return wave(std::integral_constant<int, 2>{});
         return wave(std::integral_constant<int, 1>{});
     }
+    if (a.N == 1) a.part_loss = loss;
     if constexpr (STATS) {
         const auto row = [&](auto u, int threads) {
             hipLaunchKernelGGL((policy_row_kernel<T, decltype(u)::value, GRAD>), dim3((unsigned)a.N), dim3(threads), 0, s, a);
@@ -603,26 +608,27 @@ template <class T, bool STATS, bool GRAD> int64_t launch_rows_of(const PolicyArg
     hipLaunchKernelGGL((policy_stream_kernel<T, STATS, GRAD>), dim3((unsigned)a.N), dim3(units <= 256 ? 64 : units <= 2048 ? 256 : 1024), 0, s, a);
     return a.N;
 }
-template <bool STATS, bool GRAD> ssm_status launch_rows(const PolicyArgs &a, int dtype, float *loss, hipStream_t s)
+template <bool STATS, bool GRAD> ssm_status launch_rows(PolicyArgs &a, int dtype, float *loss, hipStream_t s)
 {
     const int64_t units = ((int64_t)a.K * (int64_t)dtype_bytes(dtype) + 15) / 16;
     const int count = pieces_of(a.N, units);
     if (count && (STATS || a.dlogits != a.logits)) {
         Pieces c{(int)((units + count - 1) / count), count, STATS ? a.part_loss + PIECES_MAX_ROWS : nullptr, nullptr};
         if (STATS) c.xa = c.sums + 3 * a.N * count;
+        if (STATS && a.N == 1) a.part_loss = loss;
         const dim3 grid((unsigned)(a.N * count));
         with_dtype(dtype, [&](auto t) {
             using T = decltype(t);
             if constexpr (STATS) hipLaunchKernelGGL(policy_piece_kernel<T>, grid, dim3(256), 0, s, a, c);
             if constexpr (GRAD) hipLaunchKernelGGL((policy_piece_gradient_kernel<T, !STATS>), grid, dim3(256), 0, s, a, c);
         });
-        if constexpr (STATS && GRAD) hipLaunchKernelGGL(policy_sum_kernel, dim3(1), dim3(64), 0, s, a.part_loss, a.N, loss);
+        if constexpr (STATS && GRAD) { if (a.N > 1) hipLaunchKernelGGL(policy_sum_kernel, dim3(1), dim3(64), 0, s, a.part_loss, a.N, loss); }
         else if constexpr (STATS) hipLaunchKernelGGL(policy_join_kernel, dim3(1), dim3(64), 0, s, a, c, loss);
         return hipGetLastError() == hipSuccess ? SSM_OK : SSM_ERR_HIP;
     }
-    const int64_t parts = with_dtype(dtype, [&](auto t) { return launch_rows_of<decltype(t), STATS, GRAD>(a, s); });
+    const int64_t parts = with_dtype(dtype, [&](auto t) { return launch_rows_of<decltype(t), STATS, GRAD>(a, loss, s); });
     if (hipGetLastError() != hipSuccess) return SSM_ERR_HIP;
-    if constexpr (STATS) {
+    if (STATS && parts > 1) {
         hipLaunchKernelGGL(policy_sum_kernel, dim3(1), dim3(parts <= 256 ? 256 : 1024), 0, s, a.part_loss, parts, loss);
         if (hipGetLastError() != hipSuccess) return SSM_ERR_HIP;
     }
@@ -639,8 +645,8 @@ extern "C" {
 size_t ssm_policy_loss_workspace_bytes(int64_t N, int64_t K)
 {
     if (N <= 0 || K <= 0 || N > SSM_MAX_TOKENS || K > (1LL << 30) || K > SSM_MAX_ELEMS / N) return 0;
-    // parts of the loss (four wavefronts' from one row on); few rows, which may go in pieces: the pieces' sums and the actions' logits
-    const size_t floats = N <= PIECES_MAX_ROWS ? PIECES_MAX_ROWS + (3 * MAX_PIECES + 1) * (size_t)N : (size_t)N + 3;
+    // parts of the loss; few rows, which may go in pieces: the pieces' sums and the actions' logits
+    const size_t floats = N <= PIECES_MAX_ROWS ? PIECES_MAX_ROWS + (3 * MAX_PIECES + 1) * (size_t)N : (size_t)N;
     return (floats * 4 + ALIGN - 1) / ALIGN * ALIGN;
 }
 
