@@ -71,8 +71,8 @@ template <bool UP, bool R> __device__ __forceinline__ Map neighbour(const Map &m
 }
 
 // Composition over the threads along time of a chunk: within a wavefront between lanes, over wavefronts in LDS (a map per wavefront and vector of channels; the
-// flag is the same for all channels of a sequence).
-struct MapLds { f32x4 m[GATED_MAX_THREADS / 64][GATED_MAX_VECS]; int r[GATED_MAX_THREADS / 64]; };
+// flag is the same for all channels of a sequence).  `lost`: a wait of the workgroup gave up.
+struct MapLds { f32x4 m[GATED_MAX_THREADS / 64][GATED_MAX_VECS]; int r[GATED_MAX_THREADS / 64]; int lost; };
 template <bool UP, bool R> __device__ __forceinline__ Map inclusive_in_wave(Map m, int lane, int cx, int span)
 {
     const int l = lane & (span - 1);
@@ -156,14 +156,18 @@ __device__ __forceinline__ void publish2(unsigned long long *w, f32x2 v, unsigne
     publish_word(w, v[0], tag);
     publish_word(w + 1, v[1], tag);
 }
-// the map at w, or one to NaN
-__device__ __forceinline__ Map wait_map(const GatedArgs &a, const unsigned long long *w)
+__device__ __forceinline__ void give_up(const GatedArgs &a, MapLds &lds)
+{
+    atomicOr(a.err, 1u);
+    lds.lost = 1;
+}
+// the map at w
+__device__ __forceinline__ Map wait_map(const GatedArgs &a, MapLds &lds, const unsigned long long *w)
 {
     Map m;
     unsigned tag;
-    const bool got = wait_words(w, a.spin_limit, m.A, tag) && wait_words(w + 64, a.spin_limit, m.S, tag);
+    if (!(wait_words(w, a.spin_limit, m.A, tag) && wait_words(w + 64, a.spin_limit, m.S, tag))) give_up(a, lds);
     m.r = tag == 2;
-    if (!got) { atomicOr(a.err, 1u); m = {f32x2{0.f, 0.f}, f32x2{__builtin_nanf(""), __builtin_nanf("")}, 1}; }
     return m;
 }
 __device__ __forceinline__ void publish_map(unsigned long long *w, const Map &m)
@@ -180,6 +184,12 @@ template <bool UP> __device__ __forceinline__ Map compose_rows(const Place &p, M
     __syncthreads();
     return fold<UP>(lds, p.vec, p.waves, p.waves);
 }
+// m, or the map to NaN where a wait of the workgroup gave up: what it got may be anything, its flag among it, and threads of one row may differ
+__device__ __forceinline__ Map or_nan(const MapLds &lds, const Map &m)
+{
+    const f32x2 nan = {__builtin_nanf(""), __builtin_nanf("")};
+    return lds.lost ? Map{nan, nan, 1} : m;
+}
 // UP: rows in the order of time.  `chunk`: number along the direction of the scan; `total`: the chunk's map, valid where `ends`; v0: what flows into the first chunk.
 // Words of a chunk: its map [0, 128), the state behind the block that it ends [128, 192), the map of the group that it ends [192, 320).
 template <bool UP> __device__ __forceinline__ f32x2 look_back(const GatedArgs &a, const Place &p, MapLds &lds, f32x2 *s_base, int chunk, int chain, const Map &total, bool ends, f32x2 v0)
@@ -190,17 +200,17 @@ template <bool UP> __device__ __forceinline__ f32x2 look_back(const GatedArgs &a
     const bool more = chunk + 1 < a.nTB;
     if (ends && more) publish_map(mine, total);
     Map chunks = identity(), groups = identity();
-    if (chunk > group) chunks = compose_rows<UP>(p, lds, group + row < chunk ? wait_map(a, mine - (chunk - group - row) * back) : identity(), cx);
-    if (ends && more && a.groups > 1 && (chunk + 1) % R == 0) publish_map(mine + 192, after<true>(total, chunks));
+    if (chunk > group) chunks = compose_rows<UP>(p, lds, group + row < chunk ? wait_map(a, lds, mine - (chunk - group - row) * back) : identity(), cx);
+    if (ends && more && a.groups > 1 && (chunk + 1) % R == 0) publish_map(mine + 192, after<true>(total, or_nan(lds, chunks)));
     if (block > 0 && row == 0) {
         unsigned tag;
         f32x2 base;
-        if (!wait_words(mine - (chunk - block + 1) * back + 128, a.spin_limit, base, tag)) { atomicOr(a.err, 1u); base = f32x2{__builtin_nanf(""), __builtin_nanf("")}; }
+        if (!wait_words(mine - (chunk - block + 1) * back + 128, a.spin_limit, base, tag)) give_up(a, lds);
         s_base[p.vec] = base;
     }
-    if (group > block) groups = compose_rows<UP>(p, lds, block + row * R < group ? wait_map(a, mine - (chunk - block - row * R - R + 1) * back + 192) : identity(), cx);
+    if (group > block) groups = compose_rows<UP>(p, lds, block + row * R < group ? wait_map(a, lds, mine - (chunk - block - row * R - R + 1) * back + 192) : identity(), cx);
     else if (block > 0) __syncthreads();
-    const f32x2 v = apply(chunks, apply(groups, block > 0 ? s_base[p.vec] : v0));
+    const f32x2 v = apply(or_nan(lds, chunks), apply(groups, block > 0 ? s_base[p.vec] : v0));
     if (ends && more && (chunk + 1) % RB == 0) publish2(mine + 128, apply(total, v), 3);
     return v;
 }
@@ -209,10 +219,13 @@ template <bool UP> __device__ __forceinline__ f32x2 look_back(const GatedArgs &a
 // lines no difference).  Not with fewer than 64 chains, which would leave XCDs idle.  The chain of workgroup n of a round, or one past the last.
 __device__ __forceinline__ int chain_of(const GatedArgs &a, int n) { return a.per_xcd ? (n & 7) * a.per_xcd + (n >> 3) : n; }
 // the chunk of this workgroup, of those of its chain in the order in which they start
-__device__ __forceinline__ int take_ticket(const GatedArgs &a, int chain)
+__device__ __forceinline__ int take_ticket(const GatedArgs &a, MapLds &lds, int chain)
 {
     __shared__ int s_chunk;
-    if (threadIdx.x == 0) s_chunk = (int)atomicAdd(a.ticket + (int64_t)chain * SCAN_TICKET_STRIDE, 1u);
+    if (threadIdx.x == 0) {
+        s_chunk = (int)atomicAdd(a.ticket + (int64_t)chain * SCAN_TICKET_STRIDE, 1u);
+        lds.lost = 0;
+    }
     __syncthreads();
     return __builtin_amdgcn_readfirstlane(s_chunk);
 }
@@ -308,7 +321,7 @@ __global__ void __launch_bounds__(GATED_MAX_THREADS) gated_fwd_kernel(GatedArgs 
     const int chain = chain_of(a, LOOK ? (int)(blockIdx.x - a.by_round(blockIdx.x) * (unsigned)a.round) : (int)blockIdx.x);
     if (chain >= a.chains) return;
     int first = 0;
-    if constexpr (LOOK) first = take_ticket(a, chain);
+    if constexpr (LOOK) first = take_ticket(a, lds, chain);
     const Place p(a, chain);
     const int cx = 1 << a.lgcx, steps = GE * a.rows;
     const int64_t state = (int64_t)p.seq * a.D + p.ch;
@@ -380,7 +393,7 @@ __global__ void __launch_bounds__(GATED_MAX_THREADS) gated_bwd_kernel(GatedArgs 
     const int chain = chain_of(a, LOOK ? (int)(blockIdx.x - a.by_round(blockIdx.x) * (unsigned)a.round) : (int)blockIdx.x);
     if (chain >= a.chains) return;
     int first = a.nTB - 1;
-    if constexpr (LOOK) first = a.nTB - 1 - take_ticket(a, chain);
+    if constexpr (LOOK) first = a.nTB - 1 - take_ticket(a, lds_down, chain);
     Place p(a, chain);
     const int cx = 1 << a.lgcx, steps = GE * a.rows;
     const f32x2 zero = {0.f, 0.f};

@@ -219,28 +219,38 @@ def test_a_captured_graph_replays_as_the_eager_calls():
                 assert torch.equal(x[k], y[k]), k
 
 
-def test_a_wait_that_gives_up_hands_on_nan():
-    """A poll bound of zero: a chunk whose predecessor is not ready yet gives up at once.  Whatever happened, the states are right or NaN, never
-    something else, and the workspace says so."""
+@pytest.mark.parametrize("flags", ("none", "some"))
+@pytest.mark.parametrize("L", (4000, 9000))
+def test_a_wait_that_gives_up_hands_on_nan(L, flags):
+    """A poll bound of zero: a chunk whose predecessor is not ready yet gives up at once, every channel for itself.  Whatever happened, the states and gradients are
+    right or NaN, never something else, and the workspace says so."""
     import torch
     from paper_2502_20168_amd import binding, learn
-    s = _inputs(2, 4000, 64, "f32", False, "none", True)
-    ref, _ = _run(s)
-    n = learn.ssm_gated_workspace_bytes(2, 4000, 64, torch.float32, False)
+    s = _inputs(2, L, 64, "f32", False, flags, True)
+    ref, back = _run(s)
+    n = learn.ssm_gated_workspace_bytes(2, L, 64, torch.float32, False)
     assert n > 0
     ws = torch.empty(n, dtype=torch.uint8, device="cuda")
-    call = lambda: learn.ssm_gated_scan_fwd(s["gate"], s["u"], s["is_first"], s["h0"], workspace=ws)
-    old = binding.ssm_set_spin_limit(0)
-    try:
+    fwd = lambda: learn.ssm_gated_scan_fwd(s["gate"], s["u"], s["is_first"], s["h0"], workspace=ws)
+    bwd = lambda: learn.ssm_gated_scan_bwd(s["gate"], s["u"], s["is_first"], s["h0"], ref["carry"], s["dh"], s["dh_last"], workspace=ws)
+    for call, right in ((fwd, ref), (bwd, back)):
+        for _ in range(4):
+            old = binding.ssm_set_spin_limit(0)
+            try:
+                r = call()
+                status = learn.ssm_workspace_status(ws)
+            finally:
+                binding.ssm_set_spin_limit(old)
+            seen = False
+            for k, t in r.items():
+                bad = torch.isnan(t)
+                seen |= bool(bad.any())
+                assert torch.equal(t[~bad], right[k][~bad]), k
+            assert status == binding.SSM_ERR_SCAN_TIMEOUT or not seen
         r = call()
-        status = learn.ssm_workspace_status(ws)
-    finally:
-        binding.ssm_set_spin_limit(old)
-    bad = torch.isnan(r["h"])
-    assert torch.equal(r["h"][~bad], ref["h"][~bad])
-    assert status == (binding.SSM_ERR_SCAN_TIMEOUT if bad.any() else binding.SSM_OK)
-    r = call()
-    assert learn.ssm_workspace_status(ws) == binding.SSM_OK and torch.equal(r["h"], ref["h"])
+        assert learn.ssm_workspace_status(ws) == binding.SSM_OK
+        for k, t in r.items():
+            assert torch.equal(t, right[k]), k
 
 
 def test_a_workspace_too_small_is_refused():
