@@ -603,9 +603,14 @@ template <class T, bool STATS, bool GRAD> int64_t launch_rows_of(PolicyArgs &a, 
         if (units <= 256 * 8) return row(std::integral_constant<int, 8>{}, 256);
         if (units <= 512 * 8) return row(std::integral_constant<int, 8>{}, 512);
         if (units <= 512 * 16) return row(std::integral_constant<int, 16>{}, 512);
-        if (units <= 1024 * 16) return row(std::integral_constant<int, 16>{}, 1024);
+        if constexpr (GRAD && sizeof(T) == 4) { if (units <= 1024 * 16) return row(std::integral_constant<int, 16>{}, 1024); }
     }
-    hipLaunchKernelGGL((policy_stream_kernel<T, STATS, GRAD>), dim3((unsigned)a.N), dim3(units <= 256 ? 64 : units <= 2048 ? 256 : 1024), 0, s, a);
+    // Beyond, held rows leave a CU one workgroup, which loads, computes and stores in turn; two that read the row again for the gradient are faster, but for
+    // 32-bit logits. us, held and read: forward 2048 x 65536 f32 131, 95; 2048 x 131072 bf16 154, 100; 1024 x 70000 bf16 71, 36.  Loss and gradient 2048 x 131072 bf16 276, 259;
+    // 1024 x 70000 bf16 104, 69; 300 x 100000 bf16 51, 41; 2048 x 65536 f32 228, 265; 2048 x 50000 f32 185, 196.  (Forward with 512 threads and 1024: 4096 x 65536 bf16 103, 111;
+    // 1024 x 81920 f16 37, 43; 130 x 100000 bf16 14.9, 14.0; 100 x 131072 f32 18.8, 17.1.)
+    const int threads = units <= 256 ? 64 : units <= 2048 ? 256 : STATS && !GRAD && a.N >= 512 ? 512 : 1024;
+    hipLaunchKernelGGL((policy_stream_kernel<T, STATS, GRAD>), dim3((unsigned)a.N), dim3(threads), 0, s, a);
     return a.N;
 }
 template <bool STATS, bool GRAD> ssm_status launch_rows(PolicyArgs &a, int dtype, float *loss, hipStream_t s)

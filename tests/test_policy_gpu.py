@@ -63,7 +63,7 @@ def _compare(s, dtype, terms=TERMS):
 
 SHAPES = [(1, 1), (3, 2), (5, 3), (64, 7), (33, 32), (17, 33), (9, 64), (300, 65), (4, 255), (6, 256), (2, 1000), (3, 1025), (2, 2048), (7, 5003),
           (1, 16384), (2, 20001), (1, 40000), (2, 70001), (1, 140000), (1, 300001),
-          (64, 9001), (65, 9001), (40, 16400), (2, 1200003)]
+          (64, 9001), (65, 9001), (40, 16400), (2, 1200003), (66, 33000), (70, 70001), (513, 33000)]
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
@@ -73,7 +73,7 @@ def test_shapes(N, K, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-@pytest.mark.parametrize("N,K,pad", [(40, 5, 1), (11, 130, 3), (3, 3000, 7), (2, 33000, 5)])
+@pytest.mark.parametrize("N,K,pad", [(40, 5, 1), (11, 130, 3), (3, 3000, 7), (2, 33000, 5), (66, 70001, 3)])
 def test_rows_in_a_padded_array(N, K, pad, dtype):
     _compare(_inputs(N, K, dtype, pad=pad, idle=0.3), dtype)
 
@@ -171,7 +171,7 @@ def test_ratios_that_overflow():
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-@pytest.mark.parametrize("N,K", [(50, 20), (4, 700), (3, 5003), (2, 50001), (1, 200003)])
+@pytest.mark.parametrize("N,K", [(50, 20), (4, 700), (3, 5003), (2, 50001), (1, 200003), (66, 70001)])
 def test_gradient_over_the_logits(N, K, dtype):
     import torch
     from paper_2502_20168_amd import learn
