@@ -20,7 +20,7 @@ BINDS = {BIND: BIND_SOURCE, BIND_LEARN: os.path.join(CSRC, "pybind_learn.cpp")}
 SOURCES = ["products2.hip", "products3.hip", "params.hip", "block.hip", "narrow.hip", "scan.hip", "ssm_api.hip", "gemm.hip", "noalloc.hip",
            "gated.hip", "policy.hip", "adamw.hip"]
 HEADERS = [os.path.join(CSRC, h) for h in ("ssm_internal.h", "fast_div.h", "store_rule.h", "gemm_common.h", "gemm_kernel.h", "gemm_packed.h", "pk_units.h", "pack.h", "lookback.h",
-                                             "elem.h", "pybind_common.h")] + \
+                                             "elem.h", "wave.h", "pybind_common.h")] + \
           [os.path.join(os.path.dirname(HERE), "include", h) for h in ("ssm.h", "ssm_measure.h", "ssm_learn.h")]
 # packed-fp32 instructions are switched off on purpose (target feature removed for device code)
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -9,6 +9,7 @@
 // (no contraction), so that a state depends on the formula alone.
 #include "elem.h"
 #include "ssm_internal.h"
+#include "wave.h"
 
 #include <cmath>
 
@@ -18,8 +19,9 @@ namespace {
 inline bool misaligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
 
 constexpr int ADAMW_TENSORS = 48;            // tensors of a launch
-constexpr int ADAMW_CHUNK = 2048;            // elements of a workgroup: two blocks of 256 per wavefront
-static_assert(ADAMW_CHUNK % (4 * SSM_ADAMW_BLOCK) == 0, "whole blocks per wavefront");
+// Elements of a workgroup, a whole number of blocks of 256 per wavefront.
+constexpr int adamw_chunk(int bits) { return bits == 8 ? 4096 : 1024; }
+constexpr int VALUES_CHUNK = 2048;
 
 struct AdamwLaunch {
     ssm_adamw_tensor t[ADAMW_TENSORS];
@@ -41,26 +43,29 @@ __device__ __forceinline__ int find_tensor(const unsigned *first, int count)
     return k;
 }
 
-// Codes.  m: 3 mantissa bits below a bias of 7, largest 448; sqrt(v): 4 below a bias of 15, largest 1.9375.
-template <int MANTISSA, int BIAS> struct Code {
-    static constexpr float DOWN = BIAS == 7 ? 0x1p-120f : 0x1p-112f, UP = BIAS == 7 ? 0x1p120f : 0x1p112f;
-    static __device__ __forceinline__ unsigned of(float magnitude)
-    {
-        const unsigned b = __float_as_uint(magnitude * DOWN), drop = 23 - MANTISSA;
-        return (b + ((1u << (drop - 1)) - 1u) + ((b >> drop) & 1u)) >> drop;
-    }
-    static __device__ __forceinline__ float value(unsigned code) { return __uint_as_float(code << (23 - MANTISSA)) * UP; }
-};
-typedef Code<3, 7> MCode;
-typedef Code<4, 15> RCode;
-constexpr float M_TOP = 448.f, R_TOP = 1.9375f, SCALE_FLOOR = 0x1p-100f;
-
-__device__ __forceinline__ unsigned wave_max_bits(unsigned v)
+// Codes of sqrt(v): 4 mantissa bits below a bias of 15, largest 1.9375.  Those of m (3 below a bias of 7, largest 448) come from the hardware's conversion, two at a time, which
+// rounds to nearest even and knows the denormal ones.
+constexpr float R_DOWN = 0x1p-112f, R_UP = 0x1p112f;
+__device__ __forceinline__ unsigned root_code(float magnitude)
 {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v = max(v, (unsigned)__shfl_xor((int)v, o));
-    return v;
+    const unsigned b = __float_as_uint(magnitude * R_DOWN), drop = 19;
+    return (b + ((1u << (drop - 1)) - 1u) + ((b >> drop) & 1u)) >> drop;
 }
+__device__ __forceinline__ float root_value(unsigned code) { return __uint_as_float(code << 19) * R_UP; }
+// (by hand: the conversion takes the code above the largest for NaN, here it is 480 like any other)
+__device__ __forceinline__ f32x4 m_values(unsigned codes)
+{
+    f32x4 m;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) m[e] = __uint_as_float((unsigned)((int)(codes << (24 - 8 * e)) >> 4) & 0x87f00000u) * 0x1p120f;
+    return m;
+}
+__device__ __forceinline__ unsigned m_codes(f32x4 m)
+{
+    return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(m[2], m[3], __builtin_amdgcn_cvt_pk_fp8_f32(m[0], m[1], 0, false), true);
+}
+__device__ __forceinline__ unsigned wave_max(unsigned v) { return over_group(v, 6, [](unsigned a, unsigned b) { return max(a, b); }); }
+constexpr float M_TOP = 448.f, R_TOP = 1.9375f, SCALE_FLOOR = 0x1p-100f;
 
 template <class T> __device__ __forceinline__ f32x4 load_upto4(const T *p, int n)
 {
@@ -92,11 +97,6 @@ __device__ __forceinline__ void store_bytes(uint8_t *p, int n, unsigned v)
 #pragma unroll
     for (int k = 0; k < 3; ++k) if (k < n) p[k] = (uint8_t)(v >> (8 * k));
 }
-__device__ __forceinline__ float m_value(unsigned code, float scale)
-{
-    const float v = MCode::value(code & 127u) * scale;
-    return code & 128u ? -v : v;
-}
 
 template <class P, class G, int BITS>
 __global__ void __launch_bounds__(256) adamw_kernel(AdamwLaunch a)
@@ -109,8 +109,8 @@ __global__ void __launch_bounds__(256) adamw_kernel(AdamwLaunch a)
     P *param = static_cast<P *>(t.param);
     const G *grad = static_cast<const G *>(t.grad);
 #pragma unroll
-    for (int j = 0; j < ADAMW_CHUNK / (4 * SSM_ADAMW_BLOCK); ++j) {
-        const int64_t at = (int64_t)(blockIdx.x - a.first[k]) * ADAMW_CHUNK + (j * 4 + wave) * SSM_ADAMW_BLOCK + lane * 4;
+    for (int j = 0; j < adamw_chunk(BITS) / (4 * SSM_ADAMW_BLOCK); ++j) {
+        const int64_t at = (int64_t)(blockIdx.x - a.first[k]) * adamw_chunk(BITS) + (j * 4 + wave) * SSM_ADAMW_BLOCK + lane * 4;
         const int64_t left = t.n - at;
         const int n = left >= 4 ? 4 : left > 0 ? (int)left : 0;
         const int64_t block = at / SSM_ADAMW_BLOCK;
@@ -123,10 +123,11 @@ __global__ void __launch_bounds__(256) adamw_kernel(AdamwLaunch a)
         } else {
             const unsigned mc = load_bytes(static_cast<uint8_t *>(t.m) + at, n), vc = load_bytes(static_cast<uint8_t *>(t.v) + at, n);
             const float ms = t.m_scale[block], vs = t.v_scale[block];
+            m = m_values(mc);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                m[e] = m_value((mc >> (8 * e)) & 255u, ms);
-                const float r = RCode::value((vc >> (8 * e)) & 255u) * vs;
+                m[e] *= ms;
+                const float r = root_value((vc >> (8 * e)) & 255u) * vs;
                 v[e] = r * r;
             }
         }
@@ -147,24 +148,32 @@ __global__ void __launch_bounds__(256) adamw_kernel(AdamwLaunch a)
             store_upto4<float>(static_cast<float *>(t.m) + at, n, m);
             store_upto4<float>(static_cast<float *>(t.v) + at, n, v);
         } else {
+            if ((block + 1) * SSM_ADAMW_BLOCK > t.n) {           // (uniform: the last block of a tensor)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) { m[e] = e < n ? m[e] : 0.f; root[e] = e < n ? root[e] : 0.f; }
+            }
             // (as bit patterns: NaN is above infinity is above every number, so either reaches the scale)
             unsigned mb = 0, rb = 0;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                mb = max(mb, e < n ? __float_as_uint(fabsf(m[e])) : 0u);
-                rb = max(rb, e < n ? __float_as_uint(root[e]) & 0x7fffffffu : 0u);
+                mb = max(mb, __float_as_uint(m[e]) & 0x7fffffffu);
+                rb = max(rb, __float_as_uint(root[e]) & 0x7fffffffu);
             }
-            const float mbig = __uint_as_float(wave_max_bits(mb)), rbig = __uint_as_float(wave_max_bits(rb));
+            const float mbig = __uint_as_float(wave_max(mb)), rbig = __uint_as_float(wave_max(rb));
             const float mk = mbig < SCALE_FLOOR ? 0.f : mbig, rk = rbig < SCALE_FLOOR ? 0.f : rbig;
-            const float mi = mk == 0.f ? 0.f : M_TOP / mk, ri = rk == 0.f ? 0.f : R_TOP / rk;
-            unsigned mc = 0, vc = 0;
+            // (both quotients in one division, in the even lanes and in the odd)
+            const bool odd = lane & 1;
+            const int over = __float_as_int((odd ? R_TOP : M_TOP) / (odd ? rk : mk));
+            const float mi = mk == 0.f ? 0.f : __int_as_float(__builtin_amdgcn_readlane(over, 0)), ri = rk == 0.f ? 0.f : __int_as_float(__builtin_amdgcn_readlane(over, 1));
+            unsigned vc = 0;
+            f32x4 scaled;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const unsigned c = MCode::of(fabsf(m[e]) * mi) & 127u;
-                mc |= (c | (__float_as_uint(m[e]) >> 31) << 7) << (8 * e);
+                scaled[e] = m[e] * mi;
                 const float y = root[e] * ri;
-                vc |= (y > 0.f ? max(RCode::of(y), 1u) & 255u : 0u) << (8 * e);
+                vc |= (y > 0.f ? max(root_code(y), 1u) & 255u : 0u) << (8 * e);
             }
+            const unsigned mc = m_codes(scaled);
             store_bytes(static_cast<uint8_t *>(t.m) + at, n, mc);
             store_bytes(static_cast<uint8_t *>(t.v) + at, n, vc);
             if (lane == 0) { t.m_scale[block] = mk * (1.f / M_TOP); t.v_scale[block] = rk * (1.f / R_TOP); }
@@ -177,17 +186,18 @@ __global__ void __launch_bounds__(256) adamw_values_kernel(ValuesLaunch a)
     const int k = find_tensor(a.first, a.count);
     const ssm_adamw_stored t = a.t[k];
 #pragma unroll
-    for (int j = 0; j < ADAMW_CHUNK / 1024; ++j) {
-        const int64_t at = (int64_t)(blockIdx.x - a.first[k]) * ADAMW_CHUNK + j * 1024 + threadIdx.x * 4;
+    for (int j = 0; j < VALUES_CHUNK / 1024; ++j) {
+        const int64_t at = (int64_t)(blockIdx.x - a.first[k]) * VALUES_CHUNK + j * 1024 + threadIdx.x * 4;
         const int64_t left = t.n - at, block = at / SSM_ADAMW_BLOCK;
         if (left <= 0) break;
         const int n = left >= 4 ? 4 : (int)left;
         const unsigned mc = load_bytes(static_cast<const uint8_t *>(t.m) + at, n), vc = load_bytes(static_cast<const uint8_t *>(t.v) + at, n);
-        f32x4 m, v;
+        const float ms = t.m_scale[block], vs = t.v_scale[block];
+        f32x4 m = m_values(mc), v;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            m[e] = m_value((mc >> (8 * e)) & 255u, t.m_scale[block]);
-            const float r = RCode::value((vc >> (8 * e)) & 255u) * t.v_scale[block];
+            m[e] *= ms;
+            const float r = root_value((vc >> (8 * e)) & 255u) * vs;
             v[e] = r * r;
         }
         if (t.m_out) store_upto4<float>(t.m_out + at, n, m);
@@ -196,7 +206,7 @@ __global__ void __launch_bounds__(256) adamw_values_kernel(ValuesLaunch a)
 }
 
 // Launches `kernel(launch)` over all tensors, ADAMW_TENSORS at a time; empty ones take no place.
-template <class L, class D, class K> ssm_status launch_all(L &a, const D *tensors, int64_t count, hipStream_t s, K kernel)
+template <class L, class D, class K> ssm_status launch_all(L &a, const D *tensors, int64_t count, int chunk, hipStream_t s, K kernel)
 {
     int64_t blocks = 0;
     a.count = 0;
@@ -208,7 +218,7 @@ template <class L, class D, class K> ssm_status launch_all(L &a, const D *tensor
     };
     for (int64_t i = 0; i < count; ++i) {
         if (tensors[i].n == 0) continue;
-        const int64_t mine = (tensors[i].n + ADAMW_CHUNK - 1) / ADAMW_CHUNK;
+        const int64_t mine = (tensors[i].n + chunk - 1) / chunk;
         if (a.count == ADAMW_TENSORS || blocks + mine > 0x7fffffffLL) { if (flush() != hipSuccess) return SSM_ERR_HIP; }
         a.t[a.count] = tensors[i];
         a.first[a.count++] = (unsigned)blocks;
@@ -219,7 +229,7 @@ template <class L, class D, class K> ssm_status launch_all(L &a, const D *tensor
 
 template <class P, class G, int BITS> ssm_status run_step(AdamwLaunch &a, const ssm_adamw_tensor *tensors, int64_t count, hipStream_t s)
 {
-    return launch_all(a, tensors, count, s, [](dim3 grid, const AdamwLaunch &l, hipStream_t st) {
+    return launch_all(a, tensors, count, adamw_chunk(BITS), s, [](dim3 grid, const AdamwLaunch &l, hipStream_t st) {
         hipLaunchKernelGGL((adamw_kernel<P, G, BITS>), grid, dim3(256), 0, st, l);
     });
 }
@@ -278,7 +288,7 @@ ssm_status ssm_adamw_values(const ssm_adamw_stored *tensors, int64_t count, void
             return SSM_ERR_INVALID_ARG;
     }
     ValuesLaunch a{};
-    return launch_all(a, tensors, count, static_cast<hipStream_t>(stream), [](dim3 grid, const ValuesLaunch &l, hipStream_t st) {
+    return launch_all(a, tensors, count, VALUES_CHUNK, static_cast<hipStream_t>(stream), [](dim3 grid, const ValuesLaunch &l, hipStream_t st) {
         hipLaunchKernelGGL(adamw_values_kernel, grid, dim3(256), 0, st, l);
     });
 }

@@ -6,6 +6,7 @@
 // c = w (eta entropy - g): one exponential and two products per logit.
 #include "elem.h"
 #include "ssm_internal.h"
+#include "wave.h"
 
 #include <type_traits>
 
@@ -30,31 +31,6 @@ struct PolicyArgs {
     float mean_weight;                       // of a row where none are given
 };
 
-// Over groups of 2^lanes neighbouring lanes, the result in all of them, without a trip through LDS: lanes exchange within four, within eight and sixteen by mirroring
-// (their fours and eights hold one value by then), rows of sixteen and halves of the wavefront by swaps.
-template <int CONTROL> __device__ __forceinline__ float exchanged(float v)
-{
-    const int x = __builtin_bit_cast(int, v);
-    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(x, x, CONTROL, 0xf, 0xf, false));
-}
-template <class F> __device__ __forceinline__ float over_group(float v, int lanes, F op)
-{
-    if (lanes >= 1) v = op(v, exchanged<0xb1>(v));           // quad_perm 1 0 3 2
-    if (lanes >= 2) v = op(v, exchanged<0x4e>(v));           // quad_perm 2 3 0 1
-    if (lanes >= 3) v = op(v, exchanged<0x141>(v));          // row_half_mirror
-    if (lanes >= 4) v = op(v, exchanged<0x140>(v));          // row_mirror
-    if (lanes >= 5) {
-        const unsigned x = __float_as_uint(v);
-        const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-        v = op(__uint_as_float(r[0]), __uint_as_float(r[1]));
-    }
-    if (lanes >= 6) {
-        const unsigned x = __float_as_uint(v);
-        const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
-        v = op(__uint_as_float(r[0]), __uint_as_float(r[1]));
-    }
-    return v;
-}
 __device__ __forceinline__ float group_sum(float v, int lanes) { return over_group(v, lanes, [](float a, float b) { return a + b; }); }
 __device__ __forceinline__ float group_max(float v, int lanes) { return over_group(v, lanes, [](float a, float b) { return fmaxf(a, b); }); }
 __device__ __forceinline__ float wave_sum(float v) { return group_sum(v, 6); }
