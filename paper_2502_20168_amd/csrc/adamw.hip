@@ -3,10 +3,14 @@
 // One pass over parameters, gradients and states.  The tensors of a launch are described in its arguments (no table in memory that would have to be
 // copied and kept); a workgroup finds its tensor among them by counting the first workgroups that are not behind its own.
 //
-// 8 bits: a wavefront holds a block of 256 elements, four to a lane, so the block's largest magnitudes are maxima over its lanes.  Codes are the
+// 8 bits: a wavefront holds a block of 256 elements, four to a lane, so the block's largest magnitudes are maxima over its lanes.  Codes of sqrt(v) are the
 // upper bits of the value as a float whose exponent was moved to the bottom of the range by one exact product: rounding to nearest even is an
 // integer addition there, and small codes become that format's denormal numbers by themselves.  What is rounded to a code is computed in single operations
 // (no contraction), so that a state depends on the formula alone.
+//
+// 32 bits: 28 bytes an element with f32 parameters, bound by memory: 2^21 x 48 elements in 522 us, 5.4 TB/s, where a large copy reaches 5.0.  8 bits: 14 bytes (f32, gradients bf16)
+// 306 us, 4.6 TB/s; 10 (all bf16) 238 us, 4.3 TB/s: some 75 instructions an element, the exact root and quotient 25 of them, leave little time beside the memory's.
+// (With codes put together by integers and maxima through LDS 337 and 306 us.)
 #include "elem.h"
 #include "ssm_internal.h"
 #include "wave.h"
@@ -19,7 +23,9 @@ namespace {
 inline bool misaligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
 
 constexpr int ADAMW_TENSORS = 48;            // tensors of a launch
-// Elements of a workgroup, a whole number of blocks of 256 per wavefront.
+// Elements of a workgroup, a whole number of blocks of 256 per wavefront.  48 tensors of 2^21 elements, us, with 1024, 2048, 4096 of them: states in 32 bits, f32 523, 547, 548,
+// bf16 400, 430, 445 (bound by memory: short workgroups keep loads and stores mixed); in 8 bits, parameters f32 and gradients bf16 410, 326, 319, both bf16 383, 302, 286 (a workgroup's
+// start counts, finding its tensor in particular).
 constexpr int adamw_chunk(int bits) { return bits == 8 ? 4096 : 1024; }
 constexpr int VALUES_CHUNK = 2048;
 
@@ -67,61 +73,57 @@ __device__ __forceinline__ unsigned m_codes(f32x4 m)
 __device__ __forceinline__ unsigned wave_max(unsigned v) { return over_group(v, 6, [](unsigned a, unsigned b) { return max(a, b); }); }
 constexpr float M_TOP = 448.f, R_TOP = 1.9375f, SCALE_FLOOR = 0x1p-100f;
 
-template <class T> __device__ __forceinline__ f32x4 load_upto4(const T *p, int n)
+template <bool FULL, class T> __device__ __forceinline__ f32x4 load_upto4(const T *p, int n)
 {
-    if (n >= 4) return widened4<T>(load_pack<T, 4>(p));
+    if (FULL || n >= 4) return widened4<T>(load_pack<T, 4>(p));
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int k = 0; k < 3; ++k) if (k < n) v[k] = (float)p[k];
     return v;
 }
-template <class T> __device__ __forceinline__ void store_upto4(T *p, int n, f32x4 v)
+template <bool FULL, class T> __device__ __forceinline__ void store_upto4(T *p, int n, f32x4 v)
 {
-    if (n >= 4) { store_pack<T, 4>(p, rounded4<T>(v)); return; }
+    if (FULL || n >= 4) { store_pack<T, 4>(p, rounded4<T>(v)); return; }
 #pragma unroll
     for (int k = 0; k < 3; ++k) if (k < n) p[k] = rounded<T>(v[k]);
 }
-__device__ __forceinline__ unsigned load_bytes(const uint8_t *p, int n)
+template <bool FULL> __device__ __forceinline__ unsigned load_bytes(const uint8_t *p, int n)
 {
     typedef unsigned loose __attribute__((aligned(1)));
-    if (n >= 4) return *reinterpret_cast<const loose *>(p);
+    if (FULL || n >= 4) return *reinterpret_cast<const loose *>(p);
     unsigned v = 0;
 #pragma unroll
     for (int k = 0; k < 3; ++k) if (k < n) v |= (unsigned)p[k] << (8 * k);
     return v;
 }
-__device__ __forceinline__ void store_bytes(uint8_t *p, int n, unsigned v)
+template <bool FULL> __device__ __forceinline__ void store_bytes(uint8_t *p, int n, unsigned v)
 {
     typedef unsigned loose __attribute__((aligned(1)));
-    if (n >= 4) { *reinterpret_cast<loose *>(p) = v; return; }
+    if (FULL || n >= 4) { *reinterpret_cast<loose *>(p) = v; return; }
 #pragma unroll
     for (int k = 0; k < 3; ++k) if (k < n) p[k] = (uint8_t)(v >> (8 * k));
 }
 
-template <class P, class G, int BITS>
-__global__ void __launch_bounds__(256) adamw_kernel(AdamwLaunch a)
+// The chunk from element `start` on.  FULL: none of it is past the end.
+template <class P, class G, int BITS, bool FULL>
+__device__ __forceinline__ void step_chunk(const AdamwLaunch &a, const ssm_adamw_tensor &t, int64_t start, float gs)
 {
-    if (a.skip && a.skip[0] != 0.f) return;
-    const int k = find_tensor(a.first, a.count);
-    const ssm_adamw_tensor t = a.t[k];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const float gs = a.grad_scale ? a.grad_scale[0] : 1.f;
     P *param = static_cast<P *>(t.param);
     const G *grad = static_cast<const G *>(t.grad);
 #pragma unroll
     for (int j = 0; j < adamw_chunk(BITS) / (4 * SSM_ADAMW_BLOCK); ++j) {
-        const int64_t at = (int64_t)(blockIdx.x - a.first[k]) * adamw_chunk(BITS) + (j * 4 + wave) * SSM_ADAMW_BLOCK + lane * 4;
+        const int64_t at = start + (j * 4 + wave) * SSM_ADAMW_BLOCK + lane * 4;
         const int64_t left = t.n - at;
-        const int n = left >= 4 ? 4 : left > 0 ? (int)left : 0;
+        const int n = FULL || left >= 4 ? 4 : left > 0 ? (int)left : 0;
         const int64_t block = at / SSM_ADAMW_BLOCK;
-        const bool live = block * SSM_ADAMW_BLOCK < t.n;         // (uniform over the wavefront)
-        if (!live) break;
-        f32x4 p = load_upto4<P>(param + at, n), g = load_upto4<G>(grad + at, n), m, v;
+        if (!FULL && block * SSM_ADAMW_BLOCK >= t.n) break;      // (uniform over the wavefront)
+        f32x4 p = load_upto4<FULL, P>(param + at, n), g = load_upto4<FULL, G>(grad + at, n), m, v;
         if constexpr (BITS == 32) {
-            m = load_upto4<float>(static_cast<float *>(t.m) + at, n);
-            v = load_upto4<float>(static_cast<float *>(t.v) + at, n);
+            m = load_upto4<FULL, float>(static_cast<float *>(t.m) + at, n);
+            v = load_upto4<FULL, float>(static_cast<float *>(t.v) + at, n);
         } else {
-            const unsigned mc = load_bytes(static_cast<uint8_t *>(t.m) + at, n), vc = load_bytes(static_cast<uint8_t *>(t.v) + at, n);
+            const unsigned mc = load_bytes<FULL>(static_cast<uint8_t *>(t.m) + at, n), vc = load_bytes<FULL>(static_cast<uint8_t *>(t.v) + at, n);
             const float ms = t.m_scale[block], vs = t.v_scale[block];
             m = m_values(mc);
 #pragma unroll
@@ -143,12 +145,12 @@ __global__ void __launch_bounds__(256) adamw_kernel(AdamwLaunch a)
                 p[e] = p[e] * a.decay - a.rate * (m[e] / (root[e] * a.inv_root2 + a.eps));
             }
         }
-        store_upto4<P>(param + at, n, p);
+        store_upto4<FULL, P>(param + at, n, p);
         if constexpr (BITS == 32) {
-            store_upto4<float>(static_cast<float *>(t.m) + at, n, m);
-            store_upto4<float>(static_cast<float *>(t.v) + at, n, v);
+            store_upto4<FULL, float>(static_cast<float *>(t.m) + at, n, m);
+            store_upto4<FULL, float>(static_cast<float *>(t.v) + at, n, v);
         } else {
-            if ((block + 1) * SSM_ADAMW_BLOCK > t.n) {           // (uniform: the last block of a tensor)
+            if (!FULL && (block + 1) * SSM_ADAMW_BLOCK > t.n) {           // (uniform: the last block of a tensor)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) { m[e] = e < n ? m[e] : 0.f; root[e] = e < n ? root[e] : 0.f; }
             }
@@ -174,11 +176,24 @@ __global__ void __launch_bounds__(256) adamw_kernel(AdamwLaunch a)
                 vc |= (y > 0.f ? max(root_code(y), 1u) & 255u : 0u) << (8 * e);
             }
             const unsigned mc = m_codes(scaled);
-            store_bytes(static_cast<uint8_t *>(t.m) + at, n, mc);
-            store_bytes(static_cast<uint8_t *>(t.v) + at, n, vc);
+            store_bytes<FULL>(static_cast<uint8_t *>(t.m) + at, n, mc);
+            store_bytes<FULL>(static_cast<uint8_t *>(t.v) + at, n, vc);
             if (lane == 0) { t.m_scale[block] = mk * (1.f / M_TOP); t.v_scale[block] = rk * (1.f / R_TOP); }
         }
     }
+}
+
+template <class P, class G, int BITS>
+__global__ void __launch_bounds__(256) adamw_kernel(AdamwLaunch a)
+{
+    if (a.skip && a.skip[0] != 0.f) return;
+    const int k = find_tensor(a.first, a.count);
+    const ssm_adamw_tensor t = a.t[k];
+    const float gs = a.grad_scale ? a.grad_scale[0] : 1.f;
+    const int64_t start = (int64_t)(blockIdx.x - a.first[k]) * adamw_chunk(BITS);
+    // (in 32 bits there is little arithmetic to spare, and the smaller kernel is faster: parameters bf16 403 us, with both 416)
+    if (BITS == 8 && t.n - start >= adamw_chunk(BITS)) step_chunk<P, G, BITS, true>(a, t, start, gs);
+    else step_chunk<P, G, BITS, false>(a, t, start, gs);
 }
 
 __global__ void __launch_bounds__(256) adamw_values_kernel(ValuesLaunch a)
@@ -191,7 +206,7 @@ __global__ void __launch_bounds__(256) adamw_values_kernel(ValuesLaunch a)
         const int64_t left = t.n - at, block = at / SSM_ADAMW_BLOCK;
         if (left <= 0) break;
         const int n = left >= 4 ? 4 : (int)left;
-        const unsigned mc = load_bytes(static_cast<const uint8_t *>(t.m) + at, n), vc = load_bytes(static_cast<const uint8_t *>(t.v) + at, n);
+        const unsigned mc = load_bytes<false>(static_cast<const uint8_t *>(t.m) + at, n), vc = load_bytes<false>(static_cast<const uint8_t *>(t.v) + at, n);
         const float ms = t.m_scale[block], vs = t.v_scale[block];
         f32x4 m = m_values(mc), v;
 #pragma unroll
@@ -200,8 +215,8 @@ __global__ void __launch_bounds__(256) adamw_values_kernel(ValuesLaunch a)
             const float r = root_value((vc >> (8 * e)) & 255u) * vs;
             v[e] = r * r;
         }
-        if (t.m_out) store_upto4<float>(t.m_out + at, n, m);
-        if (t.v_out) store_upto4<float>(t.v_out + at, n, v);
+        if (t.m_out) store_upto4<false, float>(t.m_out + at, n, m);
+        if (t.v_out) store_upto4<false, float>(t.v_out + at, n, v);
     }
 }
 
