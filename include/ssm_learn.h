@@ -43,7 +43,8 @@ typedef struct { int64_t seq, step; } ssm_strides;
  *   out: dgate, du [Bt,L,D], dh0 [Bt,D] f32 (NULL allowed)
  * It computes the states again from carry instead of reading h, so their rounding to 16 bits does not enter.
  * Workspace: ssm_gated_workspace_bytes(...) bytes, 256-byte aligned; 0 = this shape needs none (NULL allowed) or is invalid.
- * ssm_workspace_status applies where one is used.  Outputs must not alias inputs.                              */
+ * ssm_workspace_status applies where one is used.  Outputs must not alias inputs.  L: at most SSM_MAX_TOKENS - 8192.  (Here and below, a call whose
+ * grid would hold 2^32 threads is refused with SSM_ERR_UNSUPPORTED.)                                            */
 #define SSM_GATED_CARRY_STEPS 128
 int64_t ssm_gated_carry_rows(int64_t L);
 size_t ssm_gated_workspace_bytes(int64_t Bt, int64_t L, int64_t D, int dtype, int want_bwd);

@@ -234,7 +234,7 @@ template <class L, class D, class K> ssm_status launch_all(L &a, const D *tensor
     for (int64_t i = 0; i < count; ++i) {
         if (tensors[i].n == 0) continue;
         const int64_t mine = (tensors[i].n + chunk - 1) / chunk;
-        if (a.count == ADAMW_TENSORS || blocks + mine > 0x7fffffffLL) { if (flush() != hipSuccess) return SSM_ERR_HIP; }
+        if (a.count == ADAMW_TENSORS || !fits_a_grid(blocks + mine, 256)) { if (flush() != hipSuccess) return SSM_ERR_HIP; }
         a.t[a.count] = tensors[i];
         a.first[a.count++] = (unsigned)blocks;
         blocks += mine;
@@ -269,7 +269,7 @@ ssm_status ssm_adamw_step(const ssm_adamw_tensor *tensors, int64_t count, ssm_ad
         const ssm_adamw_tensor &t = tensors[i];
         if (t.n < 0) return SSM_ERR_INVALID_ARG;
         if (t.n == 0) continue;
-        if (t.n > SSM_MAX_ELEMS) return SSM_ERR_UNSUPPORTED;
+        if (t.n > SSM_MAX_ELEMS || !fits_a_grid((t.n + adamw_chunk(state_bits) - 1) / adamw_chunk(state_bits), 256)) return SSM_ERR_UNSUPPORTED;
         if (!t.param || !t.grad || !t.m || !t.v || misaligned(t.param, pb) || misaligned(t.grad, gb)) return SSM_ERR_INVALID_ARG;
         if (state_bits == 32 ? misaligned(t.m, 4) || misaligned(t.v, 4)
                              : !t.m_scale || !t.v_scale || misaligned(t.m_scale, 4) || misaligned(t.v_scale, 4))
@@ -298,7 +298,7 @@ ssm_status ssm_adamw_values(const ssm_adamw_stored *tensors, int64_t count, void
         const ssm_adamw_stored &t = tensors[i];
         if (t.n < 0) return SSM_ERR_INVALID_ARG;
         if (t.n == 0) continue;
-        if (t.n > SSM_MAX_ELEMS) return SSM_ERR_UNSUPPORTED;
+        if (t.n > SSM_MAX_ELEMS || !fits_a_grid((t.n + VALUES_CHUNK - 1) / VALUES_CHUNK, 256)) return SSM_ERR_UNSUPPORTED;
         if (!t.m || !t.v || !t.m_scale || !t.v_scale || misaligned(t.m_scale, 4) || misaligned(t.v_scale, 4) || misaligned(t.m_out, 4) || misaligned(t.v_out, 4))
             return SSM_ERR_INVALID_ARG;
     }

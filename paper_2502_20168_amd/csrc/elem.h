@@ -34,6 +34,9 @@ template <class T> __device__ __forceinline__ typename Pack<T, 4>::type rounded4
 }
 template <class T> __device__ __forceinline__ f32x4 widened4(typename Pack<T, 4>::type v) { return __builtin_convertvector(v, f32x4); }
 
+// A grid holds fewer than 2^31 workgroups and fewer than 2^32 threads.
+inline bool fits_a_grid(int64_t blocks, int threads) { return blocks <= 0x7fffffffLL && blocks * threads <= 0xffffffffLL; }
+
 // the host's side of a dtype argument
 inline bool dtype_known(int dtype) { return dtype == SSM_F32 || dtype == SSM_BF16 || dtype == SSM_F16; }
 inline size_t dtype_bytes(int dtype) { return dtype == SSM_F32 ? 4 : 2; }

@@ -596,13 +596,14 @@ ssm_status check_shape(int dtype, int64_t Bt, int64_t L, int64_t D)
 {
     if (Bt <= 0 || L <= 0 || D <= 0 || !dtype_known(dtype)) return SSM_ERR_INVALID_ARG;
     if (D > SSM_MAX_WIDTH || Bt > SSM_MAX_TOKENS || L > SSM_MAX_TOKENS / Bt || Bt * L > SSM_MAX_ELEMS / D) return SSM_ERR_UNSUPPORTED;
+    if (L > SSM_MAX_TOKENS - GE * GATED_MAX_THREADS) return SSM_ERR_UNSUPPORTED;          // (the last chunk's end is an int too)
     return SSM_OK;
 }
 
 ssm_status launch_gated(GatedArgs &a, bool reverse, int dtype, int linear, void *workspace, size_t ws_bytes, hipStream_t s)
 {
     const GatedPlan pl = plan_gated(a.Bt, a.L, a.D);
-    if (pl.blocks > 0x7fffffffLL) return SSM_ERR_UNSUPPORTED;
+    if (!fits_a_grid(pl.blocks, pl.threads)) return SSM_ERR_UNSUPPORTED;
     a.lgcx = pl.lgcx; a.lgspan = pl.lgspan; a.rows = pl.rows; a.seqs = pl.seqs; a.nCX = pl.nCX; a.nTB = pl.nTB;
     a.carry_rows = (int)ssm_gated_carry_rows(a.L);
     a.chains = (int)pl.chains; a.per_xcd = pl.per_xcd; a.round = (int)pl.round;
@@ -706,9 +707,9 @@ ssm_status ssm_gated_step(const void *gate, int64_t gate_pitch, const void *u, i
     if (misaligned(gate, e) || misaligned(u, e) || misaligned(y, e) || misaligned(h_prev, 4) || misaligned(h, 4) || gate_pitch < 0 || u_pitch < 0)
         return SSM_ERR_INVALID_ARG;
     if (!strides_in_range({gate_pitch, 0}, Bt, 1) || !strides_in_range({u_pitch, 0}, Bt, 1)) return SSM_ERR_UNSUPPORTED;
-    const int64_t n = Bt * D;
-    if (n > 0x7fffffffLL * 256) return SSM_ERR_UNSUPPORTED;
-    const dim3 grid((unsigned)((n + 255) / 256)), block(256);
+    const int64_t n = Bt * D, blocks = (n + 255) / 256;
+    if (!fits_a_grid(blocks, 256)) return SSM_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)blocks), block(256);
     hipStream_t s = static_cast<hipStream_t>(stream);
     with_dtype(dtype, [&](auto t) {
         using T = decltype(t);

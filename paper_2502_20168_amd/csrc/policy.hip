@@ -548,7 +548,7 @@ int pieces_of(int64_t N, int64_t units)
 }
 
 // Who holds a row: part of a wavefront, a wavefront, a workgroup, or nobody.
-// Workgroups, and so parts of the loss.  With one, its part is the loss: `a.part_loss` is where that goes then (set here), and nothing is left to add up.
+// Workgroups, and so parts of the loss; none where a grid does not hold them.  With one, its part is the loss: `a.part_loss` is where that goes then (set here), and nothing is left to add up.
 template <class T, bool STATS, bool GRAD> int64_t launch_rows_of(PolicyArgs &a, float *loss, hipStream_t s)
 {
     constexpr int V = Unit<T>::V;
@@ -559,6 +559,7 @@ template <class T, bool STATS, bool GRAD> int64_t launch_rows_of(PolicyArgs &a, 
         const auto wave = [&](auto batches) {
             constexpr int B = decltype(batches)::value;
             const int64_t rows = 4 * (64 >> lanes) * B, blocks = (a.N + rows - 1) / rows;
+            if (!fits_a_grid(blocks, 256)) return (int64_t)0;
             if (blocks == 1) a.part_loss = loss;
             hipLaunchKernelGGL((policy_wave_kernel<T, B, STATS, GRAD>), dim3((unsigned)blocks), dim3(256), 0, s, a, lanes);
             return blocks;
@@ -573,6 +574,7 @@ template <class T, bool STATS, bool GRAD> int64_t launch_rows_of(PolicyArgs &a, 
     if (a.N == 1) a.part_loss = loss;
     if constexpr (STATS) {
         const auto row = [&](auto u, int threads) {
+            if (!fits_a_grid(a.N, threads)) return (int64_t)0;
             hipLaunchKernelGGL((policy_row_kernel<T, decltype(u)::value, GRAD>), dim3((unsigned)a.N), dim3(threads), 0, s, a);
             return a.N;
         };
@@ -590,6 +592,7 @@ template <class T, bool STATS, bool GRAD> int64_t launch_rows_of(PolicyArgs &a, 
     // 1024 x 70000 bf16 104, 69; 300 x 100000 bf16 51, 41; 2048 x 65536 f32 228, 265; 2048 x 50000 f32 185, 196.  (Forward with 512 threads and 1024: 4096 x 65536 bf16 103, 111;
     // 1024 x 81920 f16 37, 43; 130 x 100000 bf16 14.9, 14.0; 100 x 131072 f32 18.8, 17.1.)
     const int threads = units <= 256 ? 64 : units <= 2048 ? 256 : STATS && !GRAD && a.N >= 512 ? 512 : 1024;
+    if (!fits_a_grid(a.N, threads)) return 0;
     hipLaunchKernelGGL((policy_stream_kernel<T, STATS, GRAD>), dim3((unsigned)a.N), dim3(threads), 0, s, a);
     return a.N;
 }
@@ -612,6 +615,7 @@ template <bool STATS, bool GRAD> ssm_status launch_rows(PolicyArgs &a, int dtype
         return hipGetLastError() == hipSuccess ? SSM_OK : SSM_ERR_HIP;
     }
     const int64_t parts = with_dtype(dtype, [&](auto t) { return launch_rows_of<decltype(t), STATS, GRAD>(a, loss, s); });
+    if (parts == 0) return SSM_ERR_UNSUPPORTED;
     if (hipGetLastError() != hipSuccess) return SSM_ERR_HIP;
     if (STATS && parts > 1) {
         hipLaunchKernelGGL(policy_sum_kernel, dim3(1), dim3(parts <= 256 ? 256 : 1024), 0, s, a.part_loss, parts, loss);

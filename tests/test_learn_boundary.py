@@ -150,6 +150,25 @@ def test_empty_tensors_alone_launch_nothing(lib):
     assert _adamw(lib, [_tensor(n=0, param=None)]) == ssm.SSM_OK
 
 
+def test_what_no_grid_holds(lib):
+    """A grid holds fewer than 2^32 threads; a sequence's last chunk ends within 31 bits."""
+    import torch
+    far = learn._Strides(1 << 40, 1)
+    for fn in ("ssm_gated_scan_fwd", "ssm_gated_scan_bwd"):
+        strides = dict(gs=far, us=far, hs=far) if fn.endswith("fwd") else dict(gs=far, us=far, dhs=far, dgs=far, dus=far)
+        assert _gated(lib, fn, Bt=1, L=(1 << 31) - 1, D=1, **strides) == BIG
+        assert _gated(lib, fn, Bt=1, L=(1 << 31) - 8192, D=1, **strides) == BIG
+    assert learn.ssm_gated_workspace_bytes(1, (1 << 31) - 1, 1, torch.float32, False) == 0
+    assert lib.ssm_gated_step(FAKE, 4, FAKE, 4, None, None, 0, 0, 1 << 20, 4097, FAKE, None, None) == BIG
+    for fn in ("ssm_policy_loss_fwd", "ssm_policy_loss_bwd", "ssm_policy_loss_grad"):
+        for N, K in ((1 << 26, 1000), (1 << 24, 9000)):
+            assert _policy(lib, fn, N=N, K=K, pitch=K, dpitch=K, n=1 << 40) == BIG, (fn, N, K)
+    for bits, chunk in ((32, 1024), (8, 4096)):
+        assert _adamw(lib, [_tensor(n=(1 << 24) * chunk)], bits=bits) == BIG
+    one = (learn._AdamwStored * 1)(learn._AdamwStored(FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, 1 << 35))
+    assert lib.ssm_adamw_values(one, 1, None) == BIG
+
+
 WRONG = {"shape": lambda t: t[..., :-1].contiguous(), "stride": lambda t: t.repeat_interleave(2, -1)[..., ::2], "device": lambda t: t.cpu(),
          "type": lambda t: t.double() if t.is_floating_point() else t.short()}
 
