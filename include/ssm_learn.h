@@ -114,7 +114,7 @@ ssm_status ssm_policy_loss_grad(const void *logits, int64_t pitch, const int64_t
  *        held, with a fourth mantissa bit in place of the sign; a positive v is never stored as zero.
  * A block's scale is its largest magnitude divided by the largest code (0 where that magnitude is below 2^-100; infinite or NaN
  * where one of them is, which makes the block NaN in the next step).  The parameter is updated from the unrounded m and v.
- *   tensors: HOST array of `count` descriptions, read during the call; n = 0 is allowed and does nothing.
+ *   tensors: HOST array of `count` descriptions, read during the call; n = 0 is allowed and does nothing; no array may overlap another.
  *   dtype of the parameters and of the gradients: equal, or parameters f32 and gradients any.
  * ssm_adamw_values writes what the 8-bit states stand for to m_out and v_out (n f32 each, either NULL when not wanted).
  * All hyperparameters are doubles; step counts from 1.                                                                     */

@@ -519,15 +519,17 @@ __global__ void __launch_bounds__(256) gated_step_kernel(const T *__restrict__ g
 
 // Vectors of channels and threads along time of a workgroup, sequences per workgroup, chunks of a sequence; look: a workgroup per chunk.
 //   A sequence whose channels fit a wavefront with all its steps shares it with others.
-//   256 chains of 64 channels and more: workgroups of 512 threads that walk the chunks of a chain.  Nothing is handed over, and whole cache lines are read at once.
-//   Fewer leave CUs idle: narrower chains (32, 16, 8 channels) in workgroups of up to 1024 threads, those that give a CU the fewest threads' work, of equal ones the widest.
-//   Forward and gradient pass, us, with 64 or 32 channels and narrower: 4 x 512 x 256 f32 6.6 and 9.8, 4.9 and 7.1 (8); 12 x 400 x 192 bf16 6.5 and 9.6, 5.5 and 7.6 (16); 1 x 100 x 64 f32
+//   More than 256 chains of 64 channels: workgroups of 512 threads that walk the chunks of a chain.  Nothing is handed over, and whole cache lines are read at once.  (A workgroup
+//   per chunk: 64 x 2048 x 512 bf16 forward and gradient pass 94 and 167 us, 122 and 171; 1024 threads: 106 and 165; 100 x 300 x 300 f32 22 and 38, 29 and 41, 31 and 46.)
+//   256 and fewer: a workgroup of up to 1024 threads for each, the chains narrower (32, 16, 8 channels) where that gives a CU fewer threads' work; of equal ones the widest.
+//   With 64 channels (32 from 256 steps on) and narrower, us: 4 x 512 x 256 f32 6.6 and 9.8, 4.9 and 7.1 (8); 12 x 400 x 192 bf16 6.5 and 9.6, 5.5 and 7.6 (16); 1 x 100 x 64 f32
 //   4.9 and 6.5, 3.9 and 5.3 (8).  Of 4 channels: 5.5 and 8.1, 7.3 and 10.8, 4.0 and 5.4.
-//   That beats a workgroup per chunk, which costs a second launch and the hand-over, as long as a CU's share is short or all CUs have one.  Per chunk and narrower:
-//   16 x 1024 x 256 f32 15.2 and 21.2, 11.7 and 18.7 (16 channels, 1 workgroup's threads); 10 x 900 x 400 bf16 15.7 and 19.9, 8.6 and 14.4 (16, 0.9);
-//   16 x 1500 x 400 f16 26.2 and 32.8, 19.2 and 30.8 (32, 2.9); 64 x 3000 x 64 bf16 29.3 and 36.7, 23.1 and 36.6 (16, 2.9).
-//   The other way round: 4 x 4096 x 256 bf16 14.3 and 17.4, 15.7 and 27.6 (8, 2, 128 chains); 16 x 3000 x 300 f32 41 and 68, 42 and 89 (32, 5.9);
-//   8 x 8192 x 512 f32 95 and 146, 110 and 182 (16, 8).
+//   That beats a workgroup per chunk, which costs a second launch and the hand-over, as long as a CU's share is short, or all CUs have one of whole cache lines.  Per chunk and
+//   so (channels, share in workgroups of 1024): 16 x 1024 x 256 f32 15.2 and 21.2, 11.7 and 18.7 (16, 1); 10 x 900 x 400 bf16 15.7 and 19.9, 8.6 and 14.4 (16, 0.9);
+//   16 x 1500 x 400 f16 26.2 and 32.8, 19.2 and 30.8 (32, 2.9); 64 x 3000 x 64 bf16 29.3 and 36.7, 23.1 and 36.6 (16, 2.9); 30 x 1024 x 512 bf16 32 and 41, 24 and 39 (64, 4, 240 chains);
+//   28 x 4096 x 512 bf16 113 and 161, 98 and 158 (64, 16, 224 chains); 16 x 4096 x 512 bf16 59 and 95, 48 and 103 (32, 8); 32 x 4096 x 512 bf16 127 and 173, 101 and 164 (64, 16; 512 threads: 120 and 183).
+//   The other way round: 4 x 4096 x 256 bf16 14.3 and 17.4, 15.7 and 27.6 (8, 2, 128 chains); 16 x 3000 x 300 f32 41 and 68, 42 and 89 (32, 5.9, 160 chains);
+//   20 x 4096 x 512 bf16 73 and 125, 72 and 151 (64, 16, 160 chains); 8 x 8192 x 512 f32 95 and 146, 110 and 182 (16, 8).
 struct GatedPlan { int lgcx, lgspan, rows, seqs, threads, nCX, nTB; bool look; int per_xcd; int64_t chains, round, blocks; size_t ticket_bytes, desc_bytes; };
 GatedPlan plan_gated(int64_t Bt, int64_t L, int64_t D)
 {
@@ -537,12 +539,13 @@ GatedPlan plan_gated(int64_t Bt, int64_t L, int64_t D)
     int most = 512 >> pl.lgcx;               // threads along time
     const auto chains_at = [&](int lg) { return Bt * ((vecs + (1 << lg) - 1) >> lg); };
     bool few = chains_at(pl.lgcx) < GATED_CUS;
-    if (few && rows << pl.lgcx > 64) {
-        const int widest = pl.lgcx < 4 ? pl.lgcx : 4, narrowest = pl.lgcx < 2 ? pl.lgcx : 2;
+    if (chains_at(pl.lgcx) <= GATED_CUS && rows << pl.lgcx > 64) {
+        const int widest = pl.lgcx, narrowest = pl.lgcx < 2 ? pl.lgcx : 2;
         const auto share = [&](int lg) { return (chains_at(lg) + GATED_CUS - 1) / GATED_CUS * (rows << lg); };     // threads' work of a CU
         int best = widest;
         for (int lg = widest - 1; lg >= narrowest && chains_at(lg + 1) < GATED_CUS; --lg) if (share(lg) < share(best)) best = lg;
-        if (share(best) <= GATED_MAX_THREADS || (share(best) <= 3 * GATED_MAX_THREADS && chains_at(best) >= GATED_CUS * 5 / 8)) {
+        if (share(best) <= GATED_MAX_THREADS || (share(best) <= 3 * GATED_MAX_THREADS && chains_at(best) >= GATED_CUS * 5 / 8) ||
+            (best >= 4 && chains_at(best) >= GATED_CUS * 7 / 8)) {
             pl.lgcx = best;
             most = GATED_MAX_THREADS >> best;
             few = false;

@@ -52,7 +52,7 @@ def _compare(s, dtype, arithmetic=ARITHMETIC):
 
 
 SHAPES = [(1, 1, 1), (2, 1, 3), (3, 2, 5), (1, 3, 2), (70, 7, 9), (4, 16, 64), (1, 127, 64), (2, 128, 66), (2, 129, 4), (1, 257, 130), (5, 300, 250),
-          (2, 1025, 16), (1, 4100, 20), (300, 5, 3), (9, 33, 257), (130, 64, 12), (1, 640, 512), (64, 1100, 40)]
+          (2, 1025, 16), (1, 4100, 20), (300, 5, 3), (9, 33, 257), (130, 64, 12), (1, 640, 512), (64, 1100, 40), (30, 300, 500), (20, 1030, 250)]
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
