@@ -141,8 +141,8 @@ struct Place {
 // its group, all at once.  With several groups to a block the last workgroup of a group publishes the map of the group, and each row fetches that of one earlier group of the
 // block; one row fetches the state behind the block before.  R groups to a block, and the state reaches every chunk in two trips up to R^2 chunks (256: 32768
 // steps); one, and it goes from group to group.  That costs less for two groups, and where the grid takes several rounds and the groups before have long ended:
-// forward and gradient of 16 x 4096 x 512 bf16 56 and 93 us, with R groups 63 and 99; of 1 x 16384 x 256 f32 21.9 and 26.4, with R groups 19.6 and 25.1; of
-// 1 x 60000 x 64 40.8 and 42.2, with R groups 24.7 and 27.5.
+// forward and gradient of 8 x 8192 x 512 f32 101 and 144 us, with R groups 105 and 149; of 1 x 16384 x 1024 bf16 42.7 and 48.7, 45.0 and 51.5; of 1 x 16384 x 256 f32 22.9 and 25.8,
+// 20.0 and 24.5; of 1 x 60000 x 64 41.5 and 42.4, 25.0 and 27.4.
 // The order of the compositions is fixed, whatever the timing: results are repeatable.  Chunks are numbered by a ticket per chain (the chunks of one
 // sequence and channel block), so that a workgroup waits for such as have started; a wait that gives up hands on NaN and says so in the workspace.
 __device__ __forceinline__ bool wait_words(const unsigned long long *w, unsigned limit, f32x2 &v, unsigned &tag)
