@@ -74,7 +74,8 @@ ssm_status ssm_gated_step(const void *gate, int64_t gate_pitch, const void *u, i
  * against a reference policy whose log-probability is logp_ref.  The gradient, for dloss = 1 or what *dloss holds:
  *     g = (rho A where the minimum is the unclipped term, else 0, negated) + kl_coef (1 - e^d)
  *     dlogits_k = weight dloss (g ([k = a] - p_k) + entropy_coef p_k (log p_k + entropy))
- * -infinity marks an action that cannot be taken (p = 0, gradient 0); the lowest number of the type does the same.
+ * -infinity marks an action that cannot be taken (p = 0, gradient 0); the lowest number of the type does the same.  Where the row's own action
+ * is one (a mask that has changed since it was taken), logp = -infinity and rho = 0; a KL term is infinite or NaN there.
  * A row with weight 0 or a negative action, and one whose logits are all -infinity, is idle: whatever its logits hold,
  * it adds nothing to the loss, its logp, entropy and gradient are 0 and its lse is -infinity, which tells the gradient pass.
  * An action >= K, +infinity and NaN among the logits of a row that counts make the row's results NaN.

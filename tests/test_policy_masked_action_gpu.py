@@ -1,0 +1,39 @@
+"""The clipped policy loss where the row's own action has a logit far below the others, or one that cannot be taken at all."""
+import numpy as np
+import pytest
+
+from tests.learn_util import check, tolerance
+from tests.test_policy_gpu import ARITHMETIC, _inputs, _oracle
+
+pytestmark = pytest.mark.gpu
+
+# a row in part of a wavefront, in one, in a workgroup's registers, read again, in pieces
+HOLDERS = [(9, 6), (9, 70), (5, 3001), (66, 70001), (4, 70001)]
+
+
+@pytest.mark.parametrize("dtype", ("f32", "bf16"))
+@pytest.mark.parametrize("eta", (0.0, 0.05))
+@pytest.mark.parametrize("N,K", HOLDERS)
+def test_own_action_at_minus_infinity(N, K, eta, dtype):
+    """rho = 0 there: no term of the ratio for a positive advantage, the lower bound's for a negative one, the entropy's as ever."""
+    import torch
+    from paper_2502_20168_amd import learn
+    terms = {"clip_low": 0.2, "clip_high": 0.3, "kl_coef": 0.0, "entropy_coef": eta}
+    s = _inputs(N, K, dtype, masked=0.2, ref=False)
+    rows = torch.tensor([0, 1, N - 1], device="cuda")
+    s["logits"][rows, s["action"][rows]] = -float("inf")
+    s["advantage"][:3] = torch.tensor([1.5, -1.5, 0.5], device="cuda")
+    ref, args = _oracle(s, 1.0, terms), tuple(s.values())
+    f = learn.ssm_policy_loss_fwd(*args, **terms)
+    g = learn.ssm_policy_loss_grad(*args, **terms)
+    b = learn.ssm_policy_loss_bwd(*args, f["logp"], f["entropy"], f["lse"], **terms)
+    assert np.isfinite(ref["loss"]) and np.all(np.isneginf(ref["logp"][rows.cpu().numpy()]))
+    finite = np.isfinite(ref["logp"])
+    for r in (f, g):
+        assert abs(float(r["loss"]) - ref["loss"]) <= ARITHMETIC * float(s["weight"].sum()) * 8
+        assert torch.isneginf(r["logp"][rows]).all()
+        check(r["logp"][torch.from_numpy(finite).cuda()], ref["logp"][finite], ARITHMETIC, "logp")
+        check(r["entropy"], ref["entropy"], ARITHMETIC, "entropy")
+        check(r["lse"], ref["lse"], ARITHMETIC, "lse")
+    for d in (g["dlogits"], b):
+        check(d, ref["dlogits"], tolerance(dtype, 3 * ARITHMETIC), "dlogits")
