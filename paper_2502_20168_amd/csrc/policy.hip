@@ -66,8 +66,8 @@ __device__ __forceinline__ Terms row_terms(const PolicyArgs &a, const Row &r, do
     const float low = 1.f - a.terms.clip_low, high = 1.f + a.terms.clip_high;
     // (0: also of an action whose logit is -infinity, whose gap is -infinity and has no rounded part)
     const float ratio = rho0 == 0.f || rho0 == INFINITY ? rho0 : fmaf(rho0, (float)(gap - (double)g), rho0);
-    // (an advantage of zero makes the term zero, also where the ratio overflows)
-    const float raw = A == 0.f ? 0.f : ratio * A, clipped = (ratio < low ? low : ratio > high ? high : ratio) * A;
+    // (an advantage of zero makes the term zero also where the ratio overflows, but not where it is NaN)
+    const float raw = A == 0.f && ratio == INFINITY ? 0.f : ratio * A, clipped = (ratio < low ? low : ratio > high ? high : ratio) * A;
     const bool held = clipped < raw;         // (a NaN is not held: it reaches the results)
     Terms t = {-(held ? clipped : raw) - a.terms.entropy_coef * entropy, held ? 0.f : -raw};
     if (a.logp_ref) {

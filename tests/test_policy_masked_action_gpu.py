@@ -37,3 +37,22 @@ def test_own_action_at_minus_infinity(N, K, eta, dtype):
         check(r["lse"], ref["lse"], ARITHMETIC, "lse")
     for d in (g["dlogits"], b):
         check(d, ref["dlogits"], tolerance(dtype, 3 * ARITHMETIC), "dlogits")
+
+
+@pytest.mark.parametrize("N,K", HOLDERS)
+def test_no_such_action_beside_an_advantage_of_zero(N, K):
+    """An action >= K makes its row NaN whatever the advantage is, and no other row."""
+    import torch
+    from paper_2502_20168_amd import learn
+    terms = {"clip_low": 0.2, "clip_high": 0.3, "kl_coef": 0.0, "entropy_coef": 0.05}
+    s = _inputs(N, K, ref=False)
+    s["action"][1], s["advantage"][1] = K, 0.0
+    args = tuple(s.values())
+    f = learn.ssm_policy_loss_fwd(*args, **terms)
+    g = learn.ssm_policy_loss_grad(*args, **terms)
+    b = learn.ssm_policy_loss_bwd(*args, f["logp"], f["entropy"], f["lse"], **terms)
+    others = [0] + list(range(2, N))
+    for r in (f, g):
+        assert torch.isnan(r["loss"]) and torch.isnan(r["logp"][1]) and torch.isfinite(r["logp"][others]).all()
+    for d in (g["dlogits"], b):
+        assert torch.isnan(d[1]).all() and torch.isfinite(d[others]).all()
