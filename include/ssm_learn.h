@@ -84,7 +84,8 @@ ssm_status ssm_gated_step(const void *gate, int64_t gate_pitch, const void *u, i
  *   out: loss [1] f32; logp, entropy, lse [N] f32
  *   ssm_policy_loss_fwd    the loss
  *   ssm_policy_loss_bwd    the gradient, from logp, entropy and lse of the forward call; dloss [1] f32 (NULL = 1); dlogits
- *                          [N,K], rows dpitch >= K apart, may be the logits themselves (dpitch = pitch then)
+ *                          [N,K], rows dpitch >= K apart, may be the logits themselves (dpitch = pitch then).  Its probabilities are off
+ *                          by up to half a unit in the last place of the smaller of |logp| and |lse|
  *   ssm_policy_loss_grad   both in one pass over the logits where a row fits a workgroup's registers, dloss given in advance
  * Workspace (fwd, grad): ssm_policy_loss_workspace_bytes(N, K) bytes, 256-byte aligned.  Sums run in one fixed order:
  * results are repeatable.                                                                                       */

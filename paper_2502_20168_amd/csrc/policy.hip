@@ -1,8 +1,8 @@
 // Clipped policy loss with a KL term and an entropy bonus, from the logits of N rows, and its gradient (gfx950).
 //
 // With m the largest logit of a row, d_k = x_k - m and e_k = exp(d_k):  s = sum e_k, t = sum e_k d_k give lse = m + log s and
-// entropy = log s - t / s, in which nothing large cancels.  Log-probabilities are (x_k - m) - log s, or (x_k - x_a) + logp in the gradient pass on its own,
-// never x_k - lse, whose rounding at logits of 10^4 would put every probability off by 10^-3.  The gradient of a row is  a_k = p_k (c + w eta log p_k) + [k = a] w g  with
+// entropy = log s - t / s, in which nothing large cancels.  Log-probabilities are (x_k - m) - log s; in the gradient pass on its own, which has lse and logp in 32 bits,
+// (x_k - x_a) + logp or x_k - lse, whichever of logp and lse is the smaller and so rounded less.  The gradient of a row is  a_k = p_k (c + w eta log p_k) + [k = a] w g  with
 // c = w (eta entropy - g): one exponential and two products per logit.
 //
 // Large calls are bound by memory where a row's registers hold it between its sums and its gradient, so that it is read once: 4096 x 65536 bf16 forward 98 us (5.5 TB/s), loss and gradient
@@ -207,14 +207,15 @@ __device__ __forceinline__ Slope finish_row(const PolicyArgs &a, int64_t n, cons
     const float w = r.weight * (a.dloss ? a.dloss[0] : 1.f), eta = w * a.terms.entropy_coef, slope = w * t.slope;
     return {q.m, (float)(-ls * 1.4426950408889634), fmaf(eta, entropy, -slope), eta * 0.69314718f, slope, (int)r.action, idle};
 }
-// The same from what the forward pass stored.  (Differences from the logit of the action, not from lse: lse is rounded by 10^-3 at logits of 10^4.)
+// The same from what the forward pass stored.  lse and logp are both rounded at their own size: the row's other logits are taken relative to lse where that is the smaller one (an own
+// action far below them, or one that cannot be taken), else relative to the logit of the action (lse is rounded by 10^-3 at logits of 10^4).  logp itself likewise.
 __device__ __forceinline__ Slope stored_row(const PolicyArgs &a, int64_t n, const Row &r, float xa)
 {
     const float lse = a.lse[n], logp = a.logp[n], entropy = a.entropy[n];
-    const Terms t = row_terms(a, r, logp, entropy);
+    const bool by_action = fabsf(logp) <= fabsf(lse);
+    const Terms t = row_terms(a, r, by_action ? (double)logp : (double)xa - (double)lse, entropy);
     const float w = r.weight * (a.dloss ? a.dloss[0] : 1.f), eta = w * a.terms.entropy_coef, slope = w * t.slope;
-    const bool taken = xa != -INFINITY;      // (else the action cannot be taken and its logit is no reference)
-    return {taken ? xa : lse, taken ? logp * LOG2E : 0.f, fmaf(eta, entropy, -slope), eta * 0.69314718f, slope, (int)r.action,
+    return {by_action ? xa : lse, by_action ? logp * LOG2E : 0.f, fmaf(eta, entropy, -slope), eta * 0.69314718f, slope, (int)r.action,
             r.idle || lse == -INFINITY};
 }
 template <class T> __device__ __forceinline__ float logit_of_action(const T *x, const Row &r, int K)

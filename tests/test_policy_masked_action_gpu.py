@@ -56,3 +56,38 @@ def test_no_such_action_beside_an_advantage_of_zero(N, K):
         assert torch.isnan(r["loss"]) and torch.isnan(r["logp"][1]) and torch.isfinite(r["logp"][others]).all()
     for d in (g["dlogits"], b):
         assert torch.isnan(d[1]).all() and torch.isfinite(d[others]).all()
+
+
+@pytest.mark.parametrize("dtype,low", [("f32", -1e4), ("f32", -1e6), ("f32", -1e9), ("f32", None), ("bf16", -1e4), ("bf16", None), ("f16", None)])
+@pytest.mark.parametrize("N,K", HOLDERS)
+def test_gradient_from_stored_statistics_where_the_own_action_is_far_below(N, K, dtype, low):
+    """Finite logits of the own action down to the type's lowest: the gradient on its own is that of the definition, and that of loss and gradient in one call."""
+    import torch
+    from paper_2502_20168_amd import learn
+    terms = {"clip_low": 0.2, "clip_high": 0.3, "kl_coef": 0.0, "entropy_coef": 0.05}
+    s = _inputs(N, K, dtype, masked=0.2, ref=False)
+    rows = torch.tensor([0, 1, N - 1], device="cuda")
+    s["logits"][rows, s["action"][rows]] = torch.finfo(s["logits"].dtype).min if low is None else low
+    s["advantage"][:3] = torch.tensor([1.5, -1.5, 0.5], device="cuda")
+    if low is not None and low >= -1e6:                      # taken where it was as unlikely: the ratio is not zero
+        s["logp_old"][0] = s["logits"][0, s["action"][0]].float()
+    ref, args = _oracle(s, 1.0, terms), tuple(s.values())
+    f = learn.ssm_policy_loss_fwd(*args, **terms)
+    g = learn.ssm_policy_loss_grad(*args, **terms)
+    b = learn.ssm_policy_loss_bwd(*args, f["logp"], f["entropy"], f["lse"], **terms)
+    assert abs(float(f["loss"]) - ref["loss"]) <= ARITHMETIC * float(s["weight"].sum()) * 8
+    for name, d in (("one call", g["dlogits"]), ("on its own", b)):
+        for n in range(min(N, 5)):                           # (row by row: no row hides behind a larger one)
+            check(d[n], ref["dlogits"][n], tolerance(dtype, 3 * ARITHMETIC), "%s, row %d" % (name, n))
+
+
+@pytest.mark.parametrize("N,K", HOLDERS)
+def test_gradient_from_stored_statistics_at_large_logits(N, K):
+    """Logits of 10^4: lse is rounded by 5e-4, the logit of an ordinary own action is the reference."""
+    from paper_2502_20168_amd import learn
+    terms = {"clip_low": 0.2, "clip_high": 0.3, "kl_coef": 0.0, "entropy_coef": 0.05}
+    s = _inputs(N, K, ref=False)
+    s["logits"] += 1e4
+    ref, args = _oracle(s, 1.0, terms), tuple(s.values())
+    f = learn.ssm_policy_loss_fwd(*args, **terms)
+    check(learn.ssm_policy_loss_bwd(*args, f["logp"], f["entropy"], f["lse"], **terms), ref["dlogits"], tolerance("f32", 3 * ARITHMETIC), "dlogits")
