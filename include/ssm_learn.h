@@ -80,7 +80,7 @@ ssm_status ssm_gated_step(const void *gate, int64_t gate_pitch, const void *u, i
  * it adds nothing to the loss, its logp, entropy and gradient are 0 and its lse is -infinity, which tells the gradient pass.
  * An action >= K, +infinity and NaN among the logits of a row that counts make the row's results NaN.
  *   in : logits [N,K], rows `pitch` elements apart, action [N] i64, logp_old, advantage [N] f32, weight [N] f32 (NULL =
- *        1/N each), logp_ref [N] f32 (NULL = no KL term)
+ *        1/N each), logp_ref [N] f32 (NULL, or kl_coef 0: no KL term)
  *   out: loss [1] f32; logp, entropy, lse [N] f32
  *   ssm_policy_loss_fwd    the loss
  *   ssm_policy_loss_bwd    the gradient, from logp, entropy and lse of the forward call; dloss [1] f32 (NULL = 1); dlogits

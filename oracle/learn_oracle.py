@@ -75,7 +75,7 @@ def policy_loss(x, action, logp_old, advantage, weight=None, logp_ref=None, clip
         clipped = min(max(rho, 1.0 - clip_low), 1.0 + clip_high) * A
         raw = rho * A if A != 0 else 0.0
         loss, g = -min(raw, clipped) - entropy_coef * H, (-raw if raw <= clipped else 0.0)
-        if logp_ref is not None:
+        if logp_ref is not None and kl_coef != 0:
             d = float(logp_ref[n]) - logp
             loss, g = loss + kl_coef * (np.expm1(d) - d), g - kl_coef * np.expm1(d)
         out["loss"] += w * loss

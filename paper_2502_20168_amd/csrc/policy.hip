@@ -70,7 +70,7 @@ __device__ __forceinline__ Terms row_terms(const PolicyArgs &a, const Row &r, do
     const float raw = A == 0.f && ratio == INFINITY ? 0.f : ratio * A, clipped = (ratio < low ? low : ratio > high ? high : ratio) * A;
     const bool held = clipped < raw;         // (a NaN is not held: it reaches the results)
     Terms t = {-(held ? clipped : raw) - a.terms.entropy_coef * entropy, held ? 0.f : -raw};
-    if (a.logp_ref) {
+    if (a.logp_ref && a.terms.kl_coef != 0.f) {              // (0 times a distance that overflows is 0)
         // e^d - 1 - d cancels to d^2 / 2: its series up to a half, whose first term left out is 1e-9 of it
         const float d = (float)((double)r.ref - logp);
         float p = 1.f / 3628800.f;

@@ -91,3 +91,24 @@ def test_gradient_from_stored_statistics_at_large_logits(N, K):
     ref, args = _oracle(s, 1.0, terms), tuple(s.values())
     f = learn.ssm_policy_loss_fwd(*args, **terms)
     check(learn.ssm_policy_loss_bwd(*args, f["logp"], f["entropy"], f["lse"], **terms), ref["dlogits"], tolerance("f32", 3 * ARITHMETIC), "dlogits")
+
+
+@pytest.mark.parametrize("low", (-1e4, -float("inf")))
+@pytest.mark.parametrize("N,K", HOLDERS)
+def test_a_reference_without_a_coefficient(N, K, low):
+    """kl_coef 0: no KL term, also where the distance from the reference overflows."""
+    import torch
+    from paper_2502_20168_amd import learn
+    terms = {"clip_low": 0.2, "clip_high": 0.3, "kl_coef": 0.0, "entropy_coef": 0.05}
+    s = _inputs(N, K, masked=0.2)
+    s["logits"][1, s["action"][1]] = low
+    args = tuple(s.values())
+    bare = args[:-1] + (None,)
+    for call in (learn.ssm_policy_loss_fwd, learn.ssm_policy_loss_grad):
+        r, want = call(*args, **terms), call(*bare, **terms)
+        assert torch.isfinite(r["loss"])
+        for k in r:
+            assert torch.equal(r[k], want[k]), k
+    b = [learn.ssm_policy_loss_bwd(*a, r["logp"], r["entropy"], r["lse"], **terms) for a in (args, bare)]
+    assert torch.isfinite(b[0]).all() and torch.equal(*b)
+    assert abs(float(r["loss"]) - _oracle(s, 1.0, terms)["loss"]) <= ARITHMETIC * float(s["weight"].sum()) * 8
