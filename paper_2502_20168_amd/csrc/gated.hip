@@ -482,9 +482,11 @@ __global__ void __launch_bounds__(GATED_MAX_THREADS) gated_bwd_kernel(GatedArgs 
                     h = fma2(f[e], prev, u[e]);
                     u[e] = prev * d[e];
                 } else {
-                    // f prev + (1 - f) u = u + f (prev - u): rounded by u's last place, which is what prev - u has anyway
+                    // (with the complement of f as it is, like the forward pass: u + f (prev - u) would round the state by u's last place, and a gate near one
+                    // hands on little of a large u.  u is pinned: its product would be kept from the maps above, in registers that are not there)
+                    asm volatile("" : "+v"(u[e]));
                     const f32x2 w = prev - u[e];
-                    h = fma2(f[e], w, u[e]);
+                    h = fma2(f[e], prev, i[e] * u[e]);
                     d[e] *= i[e];
                     u[e] = f[e] * w * d[e];
                 }
