@@ -30,7 +30,10 @@ typedef struct { int64_t seq, step; } ssm_strides;
 /* Gated linear recurrence with episode resets: every channel decays by a factor that depends on the input,
  *     f = sigmoid(gate),    h[b,t] = (is_first[b,t] ? 0 : f (.) h[b,t-1]) + (1 - f) (.) u[b,t],    h[b,-1] = h0[b]
  * or, linear != 0, with given coefficients:   h[b,t] = (is_first[b,t] ? 0 : gate (.) h[b,t-1]) + u[b,t].
- * A reset drops the state whatever it holds, infinities and NaN included.
+ * A reset drops the state whatever it holds, infinities and NaN included.  Anything else that is infinite makes what depends on it infinite or NaN.
+ * linear: coefficients of any size and sign, but steps are taken many at a time: where the product of the coefficients of consecutive steps leaves the
+ * range of f32, a state in front of them that is not zero may come out of them as infinite, NaN or zero (and what flows back through them
+ * likewise).  Coefficients of at most one in magnitude lose nothing but such tiny remainders, and a state of zero passes any of them.
  *   in : gate, u [Bt,L,D], is_first [Bt,L] u8 (NULL = no resets), h0 [Bt,D] f32 (NULL = zeros)
  *   out: h [Bt,L,D]; h_last [Bt,D] f32 = the last state, not rounded (NULL allowed), the h0 of a call that continues the
  *        sequences; carry [Bt, ssm_gated_carry_rows(L), D] f32, the states after every SSM_GATED_CARRY_STEPS steps, which the

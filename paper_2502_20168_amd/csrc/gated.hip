@@ -59,15 +59,22 @@ __device__ __forceinline__ Gate gate_of(float z)
 __device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) { return f32x2{fmaf(a[0], b[0], c[0]), fmaf(a[1], b[1], c[1])}; }
 __device__ __forceinline__ f32x2 pick2(bool c, f32x2 a, f32x2 b) { return f32x2{c ? a[0] : b[0], c ? a[1] : b[1]}; }
 
-// a map over consecutive steps: v -> A v + S, or the constant S where r.  R: whether a reset can be among the steps at all.
+// a map over consecutive steps: v -> A v + S, or the constant S where r.  R: whether a reset can be among the steps at all.  LIN: whether A is a product of given coefficients, which may
+// be infinite where every state is finite: what is zero passes such a product as zero (a sequence that starts with padding).  A step's own coefficient is no product, and
+// is multiplied as it is.
 struct Map { f32x2 A, S; int r; };
-__device__ __forceinline__ Map identity() { return {f32x2{1.f, 1.f}, f32x2{0.f, 0.f}, 0}; }
-template <bool R> __device__ __forceinline__ Map after(const Map &y, const Map &x)      // x first, then y
+template <bool LIN> __device__ __forceinline__ f32x2 through(f32x2 A, f32x2 v, f32x2 S)
 {
-    const f32x2 s = fma2(y.A, x.S, y.S);
+    const f32x2 w = fma2(A, v, S);
+    return LIN ? f32x2{v[0] == 0.f ? S[0] : w[0], v[1] == 0.f ? S[1] : w[1]} : w;
+}
+__device__ __forceinline__ Map identity() { return {f32x2{1.f, 1.f}, f32x2{0.f, 0.f}, 0}; }
+template <bool R, bool LIN> __device__ __forceinline__ Map after(const Map &y, const Map &x)      // x first, then y
+{
+    const f32x2 s = through<LIN>(y.A, x.S, y.S);
     return {y.A * x.A, R ? pick2(y.r, y.S, s) : s, R ? y.r | x.r : 0};
 }
-__device__ __forceinline__ f32x2 apply(const Map &m, f32x2 v) { return pick2(m.r, m.S, fma2(m.A, v, m.S)); }
+template <bool LIN> __device__ __forceinline__ f32x2 apply(const Map &m, f32x2 v) { return pick2(m.r, m.S, through<LIN>(m.A, v, m.S)); }
 template <bool R> __device__ __forceinline__ Map pick(bool c, const Map &a, const Map &b) { return {pick2(c, a.A, b.A), pick2(c, a.S, b.S), R ? (c ? a.r : b.r) : 0}; }
 template <bool UP, bool R> __device__ __forceinline__ Map neighbour(const Map &m, int d)
 {
@@ -78,10 +85,10 @@ template <bool UP, bool R> __device__ __forceinline__ Map neighbour(const Map &m
 // Composition over the threads along time of a chunk: within a wavefront between lanes, over wavefronts in LDS (a map per wavefront and vector of channels; the
 // flag is the same for all channels of a sequence).  `lost`: a wait of the workgroup gave up.
 struct MapLds { f32x4 m[GATED_MAX_THREADS / 64][GATED_MAX_VECS]; int r[GATED_MAX_THREADS / 64]; int lost; };
-template <bool UP, bool R> __device__ __forceinline__ Map inclusive_in_wave(Map m, int lane, int cx, int span)
+template <bool UP, bool R, bool LIN> __device__ __forceinline__ Map inclusive_in_wave(Map m, int lane, int cx, int span)
 {
     const int l = lane & (span - 1);
-    for (int d = cx; d < span; d <<= 1) m = pick<R>(UP ? l >= d : l + d < span, after<R>(m, neighbour<UP, R>(m, d)), m);
+    for (int d = cx; d < span; d <<= 1) m = pick<R>(UP ? l >= d : l + d < span, after<R, LIN>(m, neighbour<UP, R>(m, d)), m);
     return m;
 }
 template <bool UP, bool R> __device__ __forceinline__ Map exclusive_in_wave(const Map &incl, int lane, int cx, int span)
@@ -100,7 +107,7 @@ __device__ __forceinline__ Map get(const MapLds &s, int w, int c)
     return {f32x2{q[0], q[1]}, f32x2{q[2], q[3]}, s.r[w]};
 }
 // the maps of wavefronts 0 .. n-1 (UP) or waves-1 .. waves-n, the first one first.  (Four are read at a time: one by one, every step would wait for LDS.)
-template <bool UP> __device__ __forceinline__ Map fold(const MapLds &s, int c, int n, int waves)
+template <bool UP, bool LIN> __device__ __forceinline__ Map fold(const MapLds &s, int c, int n, int waves)
 {
     Map w = identity();
     for (int k0 = 0; k0 < n; k0 += 4) {
@@ -108,7 +115,7 @@ template <bool UP> __device__ __forceinline__ Map fold(const MapLds &s, int c, i
 #pragma unroll
         for (int k = 0; k < 4; ++k) { const int i = min(k0 + k, n - 1); q[k] = get(s, UP ? i : waves - 1 - i, c); }
 #pragma unroll
-        for (int k = 0; k < 4; ++k) if (k0 + k < n) w = after<true>(q[k], w);
+        for (int k = 0; k < 4; ++k) if (k0 + k < n) w = after<true, LIN>(q[k], w);
     }
     return w;
 }
@@ -181,13 +188,13 @@ __device__ __forceinline__ void publish_map(unsigned long long *w, const Map &m)
     publish2(w + 64, m.S, m.r ? 2 : 1);
 }
 // one map per row and vector of channels -> their composition, the first row's first
-template <bool UP> __device__ __forceinline__ Map compose_rows(const Place &p, MapLds &lds, Map m, int cx)
+template <bool UP, bool LIN> __device__ __forceinline__ Map compose_rows(const Place &p, MapLds &lds, Map m, int cx)
 {
-    m = inclusive_in_wave<UP, true>(m, p.lane, cx, p.span);
+    m = inclusive_in_wave<UP, true, LIN>(m, p.lane, cx, p.span);
     __syncthreads();                         // (what was in lds has been read)
     if (UP ? p.lane >= 64 - cx : p.lane < cx) put(lds, p.wave, p.vec, m);
     __syncthreads();
-    return fold<UP>(lds, p.vec, p.waves, p.waves);
+    return fold<UP, LIN>(lds, p.vec, p.waves, p.waves);
 }
 // m, or the map to NaN where a wait of the workgroup gave up: what it got may be anything, its flag among it, and threads of one row may differ
 __device__ __forceinline__ Map or_nan(const MapLds &lds, const Map &m)
@@ -197,7 +204,7 @@ __device__ __forceinline__ Map or_nan(const MapLds &lds, const Map &m)
 }
 // UP: rows in the order of time.  `chunk`: number along the direction of the scan; `total`: the chunk's map, valid where `ends`; v0: what flows into the first chunk.
 // Words of a chunk: its map [0, 128), the state behind the block that it ends [128, 192), the map of the group that it ends [192, 320).
-template <bool UP> __device__ __forceinline__ f32x2 look_back(const GatedArgs &a, const Place &p, MapLds &lds, f32x2 *s_base, int chunk, int chain, const Map &total, bool ends, f32x2 v0)
+template <bool UP, bool LIN> __device__ __forceinline__ f32x2 look_back(const GatedArgs &a, const Place &p, MapLds &lds, f32x2 *s_base, int chunk, int chain, const Map &total, bool ends, f32x2 v0)
 {
     const int cx = 1 << a.lgcx, R = a.rows, RB = R * a.groups, group = chunk / R * R, block = chunk / RB * RB, row = UP ? p.row : R - 1 - p.row;
     unsigned long long *mine = a.desc + ((int64_t)chunk * a.chains + chain) * GATED_DESC_WORDS + p.vec * GV;
@@ -205,18 +212,18 @@ template <bool UP> __device__ __forceinline__ f32x2 look_back(const GatedArgs &a
     const bool more = chunk + 1 < a.nTB;
     if (ends && more) publish_map(mine, total);
     Map chunks = identity(), groups = identity();
-    if (chunk > group) chunks = compose_rows<UP>(p, lds, group + row < chunk ? wait_map(a, lds, mine - (chunk - group - row) * back) : identity(), cx);
-    if (ends && more && a.groups > 1 && (chunk + 1) % R == 0) publish_map(mine + 192, after<true>(total, or_nan(lds, chunks)));
+    if (chunk > group) chunks = compose_rows<UP, LIN>(p, lds, group + row < chunk ? wait_map(a, lds, mine - (chunk - group - row) * back) : identity(), cx);
+    if (ends && more && a.groups > 1 && (chunk + 1) % R == 0) publish_map(mine + 192, after<true, LIN>(total, or_nan(lds, chunks)));
     if (block > 0 && row == 0) {
         unsigned tag;
         f32x2 base;
         if (!wait_words(mine - (chunk - block + 1) * back + 128, a.spin_limit, base, tag)) give_up(a, lds);
         s_base[p.vec] = base;
     }
-    if (group > block) groups = compose_rows<UP>(p, lds, block + row * R < group ? wait_map(a, lds, mine - (chunk - block - row * R - R + 1) * back + 192) : identity(), cx);
+    if (group > block) groups = compose_rows<UP, LIN>(p, lds, block + row * R < group ? wait_map(a, lds, mine - (chunk - block - row * R - R + 1) * back + 192) : identity(), cx);
     else if (block > 0) __syncthreads();
-    const f32x2 v = apply(or_nan(lds, chunks), apply(groups, block > 0 ? s_base[p.vec] : v0));
-    if (ends && more && (chunk + 1) % RB == 0) publish2(mine + 128, apply(total, v), 3);
+    const f32x2 v = apply<LIN>(or_nan(lds, chunks), apply<LIN>(groups, block > 0 ? s_base[p.vec] : v0));
+    if (ends && more && (chunk + 1) % RB == 0) publish2(mine + 128, apply<LIN>(total, v), 3);
     return v;
 }
 // Workgroups go to the eight XCDs in turn.  Neighbouring channel blocks share cache lines where rows are not whole lines (or a block is not), so
@@ -352,19 +359,19 @@ __global__ void __launch_bounds__(GATED_MAX_THREADS) gated_fwd_kernel(GatedArgs 
             constexpr bool R = decltype(r)::value;
             m = identity();
 #pragma unroll
-            for (int e = 0; e < GE; ++e) m = after<R>(Map{f[e], b[e], (int)((cut >> e) & 1u)}, m);
-            m = inclusive_in_wave<true, R>(m, p.lane, cx, p.span);
+            for (int e = 0; e < GE; ++e) m = after<R, false>(Map{f[e], b[e], (int)((cut >> e) & 1u)}, m);
+            m = inclusive_in_wave<true, R, LINEAR>(m, p.lane, cx, p.span);
             before = exclusive_in_wave<true, R>(m, p.lane, cx, p.span);
         });
         if (p.waves > 1) {                   // (uniform)
             if (p.lane >= 64 - cx) put(lds, p.wave, p.vec, m);
             __syncthreads();
-            const Map w = fold<true>(lds, p.vec, p.wave, p.waves);
-            if constexpr (LOOK) m = after<true>(m, w);
-            before = after<true>(before, w);
+            const Map w = fold<true, LINEAR>(lds, p.vec, p.wave, p.waves);
+            if constexpr (LOOK) m = after<true, LINEAR>(m, w);
+            before = after<true, LINEAR>(before, w);
         }
-        if constexpr (LOOK) in = look_back<true>(a, p, lds, s_end, tb, chain, m, p.row == a.rows - 1, in);
-        f32x2 h = apply(before, in);
+        if constexpr (LOOK) in = look_back<true, LINEAR>(a, p, lds, s_end, tb, chain, m, p.row == a.rows - 1, in);
+        f32x2 h = apply<LINEAR>(before, in);
         if (a.carry && p.stored && t0 > 0 && t0 < a.L && t0 % SSM_GATED_CARRY_STEPS == 0)
             store_channels<float, NARROW>(a.carry + ((int64_t)p.seq * a.carry_rows + t0 / SSM_GATED_CARRY_STEPS - 1) * a.D + p.ch, h);
         if_resets(plain, [&](auto r) {
@@ -443,29 +450,29 @@ __global__ void __launch_bounds__(GATED_MAX_THREADS) gated_bwd_kernel(GatedArgs 
             constexpr bool R = decltype(r)::value;
             up = identity();
 #pragma unroll
-            for (int e = 0; e < GE; ++e) up = after<R>(Map{f[e], LINEAR ? u[e] : i[e] * u[e], (int)((cut >> e) & 1u)}, up);
+            for (int e = 0; e < GE; ++e) up = after<R, false>(Map{f[e], LINEAR ? u[e] : i[e] * u[e], (int)((cut >> e) & 1u)}, up);
             down = {up.A, zero, up.r};
 #pragma unroll
             for (int e = GE - 1; e >= 0; --e) {
                 const f32x2 back = f[e] * (d[e] + down.S);
                 down.S = R ? pick2((cut >> e) & 1u, zero, back) : back;
             }
-            up = inclusive_in_wave<true, R>(up, p.lane, cx, p.span);
+            up = inclusive_in_wave<true, R, LINEAR>(up, p.lane, cx, p.span);
             before = exclusive_in_wave<true, R>(up, p.lane, cx, p.span);
-            down = inclusive_in_wave<false, R>(down, p.lane, cx, p.span);
+            down = inclusive_in_wave<false, R, LINEAR>(down, p.lane, cx, p.span);
             behind = exclusive_in_wave<false, R>(down, p.lane, cx, p.span);
         });
         if (p.waves > 1) {
             if (p.lane >= 64 - cx) put(lds_up, p.wave, p.vec, up);
             if (p.lane < cx) put(lds_down, p.wave, p.vec, down);
             __syncthreads();
-            before = after<true>(before, fold<true>(lds_up, p.vec, p.wave, p.waves));
-            const Map w = fold<false>(lds_down, p.vec, p.waves - 1 - p.wave, p.waves);
-            if constexpr (LOOK) down = after<true>(down, w);
-            behind = after<true>(behind, w);
+            before = after<true, LINEAR>(before, fold<true, LINEAR>(lds_up, p.vec, p.wave, p.waves));
+            const Map w = fold<false, LINEAR>(lds_down, p.vec, p.waves - 1 - p.wave, p.waves);
+            if constexpr (LOOK) down = after<true, LINEAR>(down, w);
+            behind = after<true, LINEAR>(behind, w);
         }
-        if constexpr (LOOK) from_right = look_back<false>(a, p, lds_down, s_end, a.nTB - 1 - tb, chain, down, p.row == 0, from_right);
-        f32x2 back = apply(behind, from_right), h = apply(before, in);
+        if constexpr (LOOK) from_right = look_back<false, LINEAR>(a, p, lds_down, s_end, a.nTB - 1 - tb, chain, down, p.row == 0, from_right);
+        f32x2 back = apply<LINEAR>(behind, from_right), h = apply<LINEAR>(before, in);
         if_resets(plain, [&](auto r) {
             constexpr bool R = decltype(r)::value;
             // chi, last step first (in place of dh)

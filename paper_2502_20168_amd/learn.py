@@ -164,7 +164,8 @@ def _given(out, name, like=None, shape=None):
 def ssm_gated_scan_fwd(gate, u, is_first=None, h0=None, *, linear: bool = False, want_carry: bool = True, workspace=None, stream=None,
                        out: Optional[Dict] = None) -> Dict[str, object]:
     """h_t = [not first_t] f_t h_{t-1} + (1 - f_t) u_t with f = sigmoid(gate); linear: [not first_t] gate_t h_{t-1} + u_t.
-    gate, u [Bt,L,D].  Returns dict(h [Bt,L,D], h_last [Bt,D] float32, carry for the gradient pass or None)."""
+    gate, u [Bt,L,D].  Returns dict(h [Bt,L,D], h_last [Bt,D] float32, carry for the gradient pass or None).  linear: a state that is not zero
+    is lost (infinite, NaN or zero) where the product of the coefficients of consecutive steps leaves the range of float32."""
     r = (_native or _bind()).gated_scan_fwd(gate, u, is_first, h0, linear, want_carry, workspace, _handle(stream), out)
     if r is not None:
         return _done(r, "ssm_gated_scan_fwd")
