@@ -202,6 +202,13 @@ def alloc_workspace(Bt, L, H, P, want_bwd, device="cuda"):
     return torch.empty(n, dtype=torch.uint8, device=device)
 
 
+def _chk_workspace(ws):
+    """The caller's workspace: its address goes to kernels, so it has to be memory of the GPU, all of its elements next to each other."""
+    if not ws.is_cuda or not ws.is_contiguous():
+        raise ValueError("workspace must be a contiguous cuda tensor, got %s strides %s on %s" % (tuple(ws.shape), tuple(ws.stride()), ws.device))
+    return ws
+
+
 def _own_workspace(ws, stream):
     """A workspace this module allocated for one call is dropped when the call returns, while its
     kernels are still queued: tell the caching allocator which stream they run on, so that the block is
@@ -262,7 +269,7 @@ def ssm_scan_fwd(Lambda, B, C, D, log_delta, u, is_first=None, x0=None, *, want_
         torch.empty((Bt, L, P), dtype=torch.complex64, device=u.device) if want_x else None)
     x_last = out.get("x_last") if out.get("x_last") is not None else (
         torch.empty((Bt, P), dtype=torch.complex64, device=u.device) if want_x_last else None)
-    ws = workspace if workspace is not None else _own_workspace(alloc_workspace(Bt, L, H, P, False, u.device), stream)
+    ws = _chk_workspace(workspace) if workspace is not None else _own_workspace(alloc_workspace(Bt, L, H, P, False, u.device), stream)
     args = [_ptr(Lambda), _ptr(B), _ptr(C), _ptr(D), _ptr(log_delta), _ptr(u), _ptr(is_first), _ptr(x0),
             Bt, L, H, P, _ptr(y), _ptr(x), _ptr(x_last), _ptr(ws), ws.numel(), _stream(stream)]
     res = {"y": y, "x": x, "x_last": x_last}
@@ -300,7 +307,7 @@ def ssm_scan_bwd(Lambda, B, C, D, log_delta, u, is_first, x0, x, dy, *, want_dx0
         "dC": get("dC", like=C), "dD": get("dD", like=D), "dlog_delta": get("dlog_delta", like=log_delta),
         "dx0": get("dx0", shape=(Bt, P), dtype=torch.complex64) if want_dx0 else None,
     }
-    ws = workspace if workspace is not None else _own_workspace(alloc_workspace(Bt, L, H, P, True, u.device), stream)
+    ws = _chk_workspace(workspace) if workspace is not None else _own_workspace(alloc_workspace(Bt, L, H, P, True, u.device), stream)
     args = [_ptr(Lambda), _ptr(B), _ptr(C), _ptr(D), _ptr(log_delta), _ptr(u), _ptr(is_first), _ptr(x0),
             Bt, L, H, P, _ptr(x), _ptr(dy), _ptr(res["du"]), _ptr(res["dLambda"]), _ptr(res["dB"]),
             _ptr(res["dC"]), _ptr(res["dD"]), _ptr(res["dlog_delta"]), _ptr(res["dx0"]),
@@ -328,7 +335,7 @@ def ssm_scan_states(A_bar, v, is_first=None, x0=None, *, want_x_last=True, works
     _chk(is_first, torch.uint8, (Bt, L), "is_first")
     _chk(x0, torch.complex64, (Bt, P), "x0")
     x_last = torch.empty((Bt, P), dtype=torch.complex64, device=v.device) if want_x_last else None
-    ws = workspace if workspace is not None else _own_workspace(alloc_workspace(Bt, L, 1, P, False, v.device), stream)
+    ws = _chk_workspace(workspace) if workspace is not None else _own_workspace(alloc_workspace(Bt, L, 1, P, False, v.device), stream)
     rc = lib().ssm_scan_states(_ptr(A_bar), _ptr(v), _ptr(is_first), _ptr(x0), Bt, L, P, _ptr(x_last),
                                _ptr(ws), ws.numel(), _stream(stream))
     if rc != SSM_OK:
@@ -372,7 +379,7 @@ def ssm_scan_states_reverse(A_bar, gx, x, is_first=None, x0=None, *, want_dx0=Tr
     _chk(x0, torch.complex64, (Bt, P), "x0")
     dA = torch.empty_like(A_bar)
     dx0 = torch.empty((Bt, P), dtype=torch.complex64, device=gx.device) if want_dx0 else None
-    ws = workspace if workspace is not None else _own_workspace(alloc_workspace(Bt, L, 1, P, True, gx.device), stream)
+    ws = _chk_workspace(workspace) if workspace is not None else _own_workspace(alloc_workspace(Bt, L, 1, P, True, gx.device), stream)
     rc = lib().ssm_scan_states_reverse(_ptr(A_bar), _ptr(gx), _ptr(x), _ptr(is_first), _ptr(x0), Bt, L, P,
                                        _ptr(dA), _ptr(dx0), _ptr(ws), ws.numel(), _stream(stream))
     if rc != SSM_OK:
@@ -507,7 +514,7 @@ def ssm_half_glu_fwd(u, W, *, want_gate=True, workspace=None, y=None, gate=None,
     _chk(W, torch.float32, (H, H), "W")
     _chk(y, torch.float32, (T, H), "y")
     _chk(gate, torch.float32, (T, H), "gate")
-    ws = workspace if workspace is not None else _own_workspace(_glu_workspace(T, H, False, u.device), stream)
+    ws = _chk_workspace(workspace) if workspace is not None else _own_workspace(_glu_workspace(T, H, False, u.device), stream)
     y = y if y is not None else torch.empty_like(u)
     if gate is None and want_gate:
         gate = torch.empty_like(u)
@@ -528,7 +535,7 @@ def ssm_half_glu_bwd(u, W, gate, dy, *, workspace=None, du=None, dW=None, stream
         _chk(t, torch.float32, (T, H), name)
     _chk(W, torch.float32, (H, H), "W")
     _chk(dW, torch.float32, (H, H), "dW")
-    ws = workspace if workspace is not None else _own_workspace(_glu_workspace(T, H, True, u.device), stream)
+    ws = _chk_workspace(workspace) if workspace is not None else _own_workspace(_glu_workspace(T, H, True, u.device), stream)
     du = du if du is not None else torch.empty_like(u)
     dW = dW if dW is not None else torch.empty_like(W)
     rc = lib().ssm_half_glu_bwd(_ptr(u), _ptr(W), _ptr(gate), _ptr(dy), T, H, _ptr(du), _ptr(dW), _ptr(ws), ws.numel(),
@@ -568,7 +575,7 @@ def ssm_block_fwd(Lambda, B, C, D, log_delta, W, u, is_first=None, x0=None, *, w
     _chk(u, torch.float32, (Bt, L, H), "u")
     _chk(is_first, torch.uint8, (Bt, L), "is_first")
     _chk(x0, torch.complex64, (Bt, P), "x0")
-    ws = workspace if workspace is not None else _own_workspace(_block_workspace(Bt, L, H, P, False, u.device), stream)
+    ws = _chk_workspace(workspace) if workspace is not None else _own_workspace(_block_workspace(Bt, L, H, P, False, u.device), stream)
     y, out = torch.empty_like(u), torch.empty_like(u)
     gate = torch.empty_like(u) if want_gate else None
     x = torch.empty((Bt, L, P), dtype=torch.complex64, device=u.device)
@@ -592,7 +599,7 @@ def ssm_block_bwd(Lambda, B, C, D, log_delta, W, u, is_first, x0, x, y, gate, do
         _chk(t, torch.float32, (Bt, L, H), name)
     _chk(x, torch.complex64, (Bt, L, P), "x")
     _chk(W, torch.float32, (H, H), "W")
-    ws = workspace if workspace is not None else _own_workspace(_block_workspace(Bt, L, H, P, True, u.device), stream)
+    ws = _chk_workspace(workspace) if workspace is not None else _own_workspace(_block_workspace(Bt, L, H, P, True, u.device), stream)
     o = {"du": torch.empty_like(u), "dLambda": torch.empty_like(Lambda), "dB": torch.empty_like(B),
          "dC": torch.empty_like(C), "dD": torch.empty_like(D), "dlog_delta": torch.empty_like(log_delta),
          "dx0": torch.empty((Bt, P), dtype=torch.complex64, device=u.device), "dW": torch.empty_like(W)}
@@ -638,7 +645,7 @@ def ssm_plan_launches(Bt: int, L: int, H: int, P: int, ws_bytes: Optional[int] =
 
 
 def ssm_workspace_status(workspace, stream=None) -> int:
-    return int(lib().ssm_workspace_status(_ptr(workspace), _stream(stream)))
+    return int(lib().ssm_workspace_status(None if workspace is None else _ptr(_chk_workspace(workspace)), _stream(stream)))
 
 
 # ------------------------------------------------------------------ convenience for tests/bench

@@ -40,7 +40,8 @@ ENTRY(scan_fwd)
     GENERAL_PATH_UNLESS(i.ok && stream_of(a[11], &ws, s) && (a[12] == Py_None || PyDict_Check(a[12])));
     const at::Tensor &u = *i.u.t;
     Workspace w(ws, ws.none ? ssm_workspace_bytes(i.Bt, i.L, i.H, i.P, 0) : 0, u);
-    bool bad = w.bad;
+    GENERAL_PATH_UNLESS(!w.bad);
+    bool bad = false;
     at::Tensor y = output(item(a[12], "y"), true, {i.Bt, i.L, i.H}, F32, u, bad);
     at::Tensor x = output(item(a[12], "x"), yes(a[8]), {i.Bt, i.L, i.P}, C64, u, bad);
     at::Tensor xl = output(item(a[12], "x_last"), yes(a[9]), {i.Bt, i.P}, C64, u, bad);
@@ -63,7 +64,8 @@ ENTRY(scan_bwd)
                         (a[13] == Py_None || PyDict_Check(a[13])));
     const at::Tensor &u = *i.u.t;
     Workspace w(ws, ws.none ? ssm_workspace_bytes(i.Bt, i.L, i.H, i.P, 1) : 0, u);
-    bool bad = w.bad;
+    GENERAL_PATH_UNLESS(!w.bad);
+    bool bad = false;
     at::Tensor du = output(item(a[13], "du"), true, {i.Bt, i.L, i.H}, F32, u, bad);
     at::Tensor dL = output(item(a[13], "dLambda"), true, {i.P}, C64, u, bad);
     at::Tensor dB = output(item(a[13], "dB"), true, {i.P, i.H}, C64, u, bad);

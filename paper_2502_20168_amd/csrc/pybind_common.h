@@ -59,6 +59,9 @@ at::Tensor output(PyObject *given, bool wanted, std::initializer_list<int64_t> s
     return wanted ? empty(shape, dt, like) : at::Tensor();
 }
 
+// A caller's workspace has to be memory of the GPU, all of its elements next to each other: its address goes to kernels.
+bool workspace_ok(const Arg &given) { return given.t && given.t->is_cuda() && given.t->is_contiguous(); }
+
 // The workspace: the caller's, or one of n bytes that lives until the call returns (its kernels are queued on the
 // stream it was allocated on, so the allocator hands the block out again behind them).
 struct Workspace {
@@ -72,7 +75,7 @@ struct Workspace {
             if (need == 0) { bad = true; return; }
             own = empty({(int64_t)need}, U8, like);
             p = own.data_ptr(); n = need;
-        } else if (given.t) {
+        } else if (workspace_ok(given)) {
             p = given.t->data_ptr(); n = (size_t)given.t->numel();
         } else {
             bad = true;

@@ -81,7 +81,8 @@ struct GatedWorkspace {
     bool bad = false;
     GatedWorkspace(const Arg &given, const Gated &i, int bwd, bool own_stream)
     {
-        if (given.t) { p = given.t->data_ptr(); n = (size_t)given.t->numel(); return; }
+        if (workspace_ok(given)) { p = given.t->data_ptr(); n = (size_t)given.t->numel(); return; }
+        if (!given.none) { bad = true; return; }
         n = ssm_gated_workspace_bytes(i.Bt, i.L, i.D, i.code, bwd);
         if (n == 0) return;
         if (!own_stream) { bad = true; return; }

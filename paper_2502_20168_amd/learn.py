@@ -9,7 +9,7 @@ from __future__ import annotations
 import ctypes
 from typing import Dict, List, Optional, Sequence, Tuple
 
-from .binding import (SSM_ERR_INVALID_ARG, SSM_ERR_UNSUPPORTED, SSM_ERR_WORKSPACE, SSM_OK, SsmError, _chk, _done, _GeneralPathOnly, _handle, _own_workspace,
+from .binding import (SSM_ERR_INVALID_ARG, SSM_ERR_UNSUPPORTED, SSM_ERR_WORKSPACE, SSM_OK, SsmError, _chk, _chk_workspace, _done, _GeneralPathOnly, _handle, _own_workspace,
                       _ptr, _stream, _torch, lib, ssm_workspace_status)
 
 __all__ = ["ssm_gated_carry_rows", "ssm_gated_workspace_bytes", "ssm_gated_scan_fwd", "ssm_gated_scan_bwd", "ssm_gated_step",
@@ -130,7 +130,7 @@ def ssm_gated_workspace_bytes(Bt: int, L: int, D: int, dtype, want_bwd: bool) ->
 
 def _gated_workspace(given, Bt, L, D, dtype, want_bwd, device, stream):
     if given is not None:
-        return given
+        return _chk_workspace(given)
     n = ssm_gated_workspace_bytes(Bt, L, D, dtype, want_bwd)
     return _own_workspace(_torch().empty(n, dtype=_torch().uint8, device=device), stream) if n else None
 
@@ -255,7 +255,7 @@ def _check_policy(logits, action, logp_old, advantage, weight, logp_ref):
 
 def _policy_workspace(given, N, K, device, stream):
     if given is not None:
-        return given
+        return _chk_workspace(given)
     n = ssm_policy_loss_workspace_bytes(N, K)
     if n == 0:
         raise SsmError(SSM_ERR_UNSUPPORTED if N > 0 and K > 0 else SSM_ERR_INVALID_ARG, "ssm_policy_loss_workspace_bytes")
