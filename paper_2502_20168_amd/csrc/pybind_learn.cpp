@@ -26,7 +26,7 @@ bool rows_ok(const Arg &a, c10::ScalarType dt, c10::IntArrayRef shape)
 }
 ssm_strides strides_of(const at::Tensor &t) { return {t.stride(0), t.stride(1)}; }
 
-// An output that lies in memory as `like` does (dense where that one has gaps), or the caller's, checked like an input.
+// An output that lies in memory as `like` does (dense where that one has gaps or overlaps itself), or the caller's, checked like an input.
 bool activation(PyObject *given, const at::Tensor &like, at::Tensor &t)
 {
     if (given && given != Py_None) {
@@ -35,8 +35,11 @@ bool activation(PyObject *given, const at::Tensor &like, at::Tensor &t)
         t = *g.t;
         return true;
     }
-    if (like.is_contiguous()) t = at::Tensor(at::detail::empty_cuda(like.sizes(), like.scalar_type(), like.device(), std::nullopt));
-    else t = at::empty_like(like);
+    if (!like.is_contiguous()) {
+        t = at::empty_like(like);
+        if (like.sizes().back() <= 1 || t.stride(-1) == 1) return true;      // (else windows over one array: empty_like has put the dimensions in another order)
+    }
+    t = at::Tensor(at::detail::empty_cuda(like.sizes(), like.scalar_type(), like.device(), std::nullopt));
     return true;
 }
 // A float32 output of this shape, or the caller's.

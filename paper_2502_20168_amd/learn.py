@@ -153,12 +153,15 @@ def _check_gated(gate, u, is_first, h0):
 
 
 def _given(out, name, like=None, shape=None):
-    """The caller's tensor of that name, or a new one: as `like` lies in memory, or float32 of `shape`."""
+    """The caller's tensor of that name, or a new one: as `like` lies in memory (dense where that one overlaps itself), or float32 of `shape`."""
     torch = _torch()
     t = out.get(name) if out else None
     if t is not None:
         return t
-    return torch.empty_like(like) if shape is None else torch.empty(shape, dtype=torch.float32, device=like.device)
+    if shape is not None:
+        return torch.empty(shape, dtype=torch.float32, device=like.device)
+    t = torch.empty_like(like)
+    return t if like.shape[-1] <= 1 or t.stride(-1) == 1 else torch.empty(like.shape, dtype=like.dtype, device=like.device)
 
 
 def ssm_gated_scan_fwd(gate, u, is_first=None, h0=None, *, linear: bool = False, want_carry: bool = True, workspace=None, stream=None,
