@@ -45,7 +45,8 @@ typedef struct { int64_t seq, step; } ssm_strides;
  *   in : the inputs of the forward call, carry from it, dh [Bt,L,D], dh_last [Bt,D] f32 (NULL = zeros)
  *   out: dgate, du [Bt,L,D], dh0 [Bt,D] f32 (NULL allowed)
  * It computes the states again from carry instead of reading h, so their rounding to 16 bits does not enter.
- * Workspace: ssm_gated_workspace_bytes(...) bytes, 256-byte aligned; 0 = this shape needs none (NULL allowed) or is invalid.
+ * Workspace: ssm_gated_workspace_bytes(...) bytes, 256-byte aligned; 0 = this shape needs none (NULL allowed) or is invalid.  (Both passes need the
+ * same: want_bwd is there as in ssm_workspace_bytes and changes nothing.)
  * ssm_workspace_status applies where one is used.  Outputs must not alias inputs.  L: at most SSM_MAX_TOKENS - 8192.  (Here and below, a call whose
  * grid would hold 2^32 threads is refused with SSM_ERR_UNSUPPORTED.)                                            */
 #define SSM_GATED_CARRY_STEPS 128

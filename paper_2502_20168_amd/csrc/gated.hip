@@ -8,8 +8,8 @@
 // to A b + G with the same A and r.
 //
 // A large call is bound by memory: three arrays forward, five back (gate and u again: the states are formed anew from fp32 ones kept every 128 steps, which costs less than reading
-// rounded ones and 1/64 of an array of them).  128 x 256 x 1024 bf16 39.4 and 74.5 us, 5.1 and 4.5 TB/s, where a copy reaches 5.0.  A small one is bound by the chain of one workgroup: loads,
-// the maps of its threads through lanes and LDS, stores (16 x 256 x 512 f32 6.0 and 10.3 us).  So a sequence is spread over as many threads as it fills, and all
+// rounded ones and 1/64 of an array of them).  128 x 256 x 1024 bf16 38.6 and 76.5 us, 5.2 and 4.4 TB/s, where a copy reaches 5.0.  A small one is bound by the chain of one workgroup: loads,
+// the maps of its threads through lanes and LDS, stores (16 x 256 x 512 f32 6.0 and 10.5 us).  So a sequence is spread over as many threads as it fills, and all
 // its loads are in flight before the first is used.
 #include "elem.h"
 #include "lookback.h"
